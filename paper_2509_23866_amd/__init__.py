@@ -22,6 +22,7 @@ import ctypes
 import importlib
 import os
 import warnings
+from typing import NamedTuple
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(HERE, "libdart.so")
@@ -49,7 +50,10 @@ EXPORTED = ("dart_tok_stats", "dart_step_select", "dart_tis_loss_fwd_bwd", "dart
             "dart_lmhead_dlogits", "dart_lmhead_dlogits_ex",
             "dart_lmhead_backward", "dart_lmhead_backward_workspace_bytes",
             "dart_lmhead_backward_ex", "dart_lmhead_backward_ex_workspace_bytes",
-            "dart_lmhead_backward_split_workspace_bytes", "dart_kept_steps",
+            "dart_lmhead_backward_split_workspace_bytes",
+            "dart_mxfp4_packed_bytes", "dart_mxfp4_scales_bytes", "dart_mxfp4_quantize",
+            "dart_mxfp4_dequantize", "dart_mxfp4_matmul", "dart_lmhead_mxfp4_tok_stats",
+            "dart_kept_steps",
             "dart_status_string")
 
 
@@ -156,6 +160,21 @@ def load_library():
         lib.dart_lmhead_backward_split_workspace_bytes.restype = ctypes.c_size_t
         lib.dart_lmhead_backward_split_workspace_bytes.argtypes = [_I64, _I64, _I64, _I64, _I64,
                                                                    ctypes.c_uint32]
+        lib.dart_mxfp4_packed_bytes.restype = ctypes.c_size_t
+        lib.dart_mxfp4_packed_bytes.argtypes = [_I64, _I64]
+        lib.dart_mxfp4_scales_bytes.restype = ctypes.c_size_t
+        lib.dart_mxfp4_scales_bytes.argtypes = [_I64, _I64]
+        lib.dart_mxfp4_quantize.restype = ctypes.c_int
+        lib.dart_mxfp4_quantize.argtypes = [_P, ctypes.c_int, _I64, _I64, _I64, _P, _P, _P]
+        lib.dart_mxfp4_dequantize.restype = ctypes.c_int
+        lib.dart_mxfp4_dequantize.argtypes = [_P, _P, _I64, _I64, ctypes.c_int, _P, _I64, _P]
+        lib.dart_mxfp4_matmul.restype = ctypes.c_int
+        lib.dart_mxfp4_matmul.argtypes = [_P, _P, _I64, _P, _P, _I64, _I64, ctypes.c_int, _P, _I64,
+                                          _P]
+        lib.dart_lmhead_mxfp4_tok_stats.restype = ctypes.c_int
+        lib.dart_lmhead_mxfp4_tok_stats.argtypes = [_P, _P, _I64, _P, _P, _I64, _I64, _P,
+                                                    ctypes.c_float, _P, _P, _P, _P,
+                                                    ctypes.c_size_t, _P]
         lib.dart_kept_steps.restype = _I64
         lib.dart_kept_steps.argtypes = [_I64, ctypes.c_double]
         lib.dart_status_string.restype = ctypes.c_char_p
@@ -882,6 +901,189 @@ def lmhead_backward_plan(T: int, V: int, budget_bytes: int = 512 << 20):
     if best is None:
         return min(T, 256), min(V, 256)
     return best[1], best[2]
+
+
+def _enqueue(name, device, stream, *args):
+    """The C call ``name`` on ``stream``, with the inputs' device current: the null stream is the
+    current device's."""
+    torch = _torch()
+    fn = getattr(load_library(), name)
+    if torch.cuda.current_device() == device.index:
+        rc = fn(*args, _stream_handle(stream, device))
+    else:
+        with torch.cuda.device(device):
+            rc = fn(*args, _stream_handle(stream, device))
+    if rc != DART_OK:
+        raise DartError(name, rc)
+
+
+def _used_on(stream, *tensors):
+    """Keeps what a call allocated itself from being handed out again before ``stream``, if it is
+    one of torch's, has passed the call."""
+    if stream is not None and hasattr(stream, "cuda_stream"):
+        for t in tensors:
+            t.record_stream(stream)
+
+
+def _out_matrix(name, out, shape, dtype, device):
+    """``out``, or a new tensor, of this shape and type, with contiguous rows that do not overlap."""
+    torch = _torch()
+    if out is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    if (not isinstance(out, torch.Tensor) or out.dtype != dtype or out.device != device
+            or tuple(out.shape) != shape or (shape[1] > 1 and out.stride(1) != 1)
+            or (shape[0] > 1 and out.stride(0) < shape[1])):
+        raise ValueError(f"{name} must be a {dtype} {shape} tensor on {device} with contiguous rows")
+    return out
+
+
+def _ld(t):
+    """The row stride of a matrix (of one row: its length)."""
+    return t.stride(0) if t.shape[0] > 1 else t.shape[1]
+
+
+_FLOATS = {"torch.float32": DART_F32, "torch.bfloat16": DART_BF16}
+
+
+class Mxfp4(NamedTuple):
+    """A rows x cols matrix in blocks of 32 four-bit values with a power-of-two scale, as
+    dart_mxfp4_quantize makes it: ``packed`` uint8 [rows, 128 ceil(cols / 256)], ``scales`` uint8
+    [dart_mxfp4_scales_bytes(rows, cols)] (include/dart.h says which byte is which)."""
+
+    packed: object
+    scales: object
+    rows: int
+    cols: int
+
+
+def dart_mxfp4_packed_bytes(R: int, K: int) -> int:
+    return int(load_library().dart_mxfp4_packed_bytes(int(R), int(K)))
+
+
+def dart_mxfp4_scales_bytes(R: int, K: int) -> int:
+    return int(load_library().dart_mxfp4_scales_bytes(int(R), int(K)))
+
+
+def _check_mxfp4(name, q, device=None):
+    torch = _torch()
+    if not isinstance(q, Mxfp4):
+        raise TypeError(f"{name} must be an Mxfp4")
+    for part, t, n in (("packed", q.packed, dart_mxfp4_packed_bytes(q.rows, q.cols)),
+                       ("scales", q.scales, dart_mxfp4_scales_bytes(q.rows, q.cols))):
+        if (not isinstance(t, torch.Tensor) or t.dtype != torch.uint8 or not t.is_contiguous()
+                or n == 0 or t.numel() != n or not t.is_cuda or t.data_ptr() % 16):
+            raise ValueError(f"{name}.{part} must be a contiguous, 16-byte aligned uint8 tensor of "
+                             f"{n} bytes on a GPU")
+        if t.device != (q.packed.device if device is None else device):
+            raise ValueError(f"{name} must be on {q.packed.device if device is None else device}")
+
+
+def dart_mxfp4_quantize(x, out=None, stream=None):
+    """The Mxfp4 of a 2-D float32 or bfloat16 tensor with contiguous rows: along a row, blocks of 32
+    values share the scale 2^max(floor(log2 of the largest size) - 2, -127), and each becomes the
+    nearest of 0, 0.5, 1, 1.5, 2, 3, 4, 6 times it (ties to the even code, larger ones 6). A block
+    with an infinity or a NaN stands for NaN. ``out``: an Mxfp4 of the same shape to write to."""
+    torch = _torch()
+    if not isinstance(x, torch.Tensor) or str(x.dtype) not in _FLOATS:
+        raise TypeError("x must be a float32 or bfloat16 tensor")
+    if x.dim() != 2 or not x.is_cuda or x.numel() == 0 or (x.shape[1] > 1 and x.stride(1) != 1):
+        raise ValueError("x must be a 2-D tensor on a GPU, not empty, with contiguous rows")
+    R, K = x.shape
+    ld = _ld(x)
+    if ld < K:
+        raise ValueError("the rows of x must not overlap")
+    if out is None:
+        packed = torch.empty((R, dart_mxfp4_packed_bytes(1, K)), dtype=torch.uint8, device=x.device)
+        scales = torch.empty(dart_mxfp4_scales_bytes(R, K), dtype=torch.uint8, device=x.device)
+        out = Mxfp4(packed, scales, R, K)
+    else:
+        _check_mxfp4("out", out, x.device)
+        if (out.rows, out.cols) != (R, K):
+            raise ValueError(f"out must be {R} x {K}")
+    _enqueue("dart_mxfp4_quantize", x.device, stream, x.data_ptr(), _FLOATS[str(x.dtype)], R, K, ld,
+             out.packed.data_ptr(), out.scales.data_ptr())
+    return out
+
+
+def dart_mxfp4_dequantize(q, dtype=None, out=None, stream=None):
+    """The values that an Mxfp4 stands for, as a [rows, cols] bfloat16 (default) or float32 tensor."""
+    torch = _torch()
+    _check_mxfp4("q", q)
+    dtype = (torch.bfloat16 if out is None else out.dtype) if dtype is None else dtype
+    if str(dtype) not in _FLOATS:
+        raise TypeError("dtype must be float32 or bfloat16")
+    out = _out_matrix("out", out, (q.rows, q.cols), dtype, q.packed.device)
+    _enqueue("dart_mxfp4_dequantize", out.device, stream, q.packed.data_ptr(), q.scales.data_ptr(),
+             q.rows, q.cols, _FLOATS[str(dtype)], out.data_ptr(), _ld(out))
+    return out
+
+
+def _as_mxfp4(name, x, stream):
+    """``x`` itself where it is an Mxfp4, else (a float32 or bfloat16 matrix) quantised."""
+    if isinstance(x, Mxfp4):
+        _check_mxfp4(name, x)
+        return x
+    q = dart_mxfp4_quantize(x, stream=stream)
+    _used_on(stream, q.packed, q.scales)
+    return q
+
+
+def dart_mxfp4_matmul(a, b, dtype=None, out=None, stream=None):
+    """a @ b^T of Mxfp4 matrices a [M, K] and b [N, K], summed in float32, as a [M, N] bfloat16
+    (default) or float32 tensor: the logits of tokens ``a`` under a head ``b`` kept in four bits.
+    ``a`` may be a float32 or bfloat16 tensor, which is quantised first."""
+    torch = _torch()
+    _check_mxfp4("b", b)
+    dtype = (torch.bfloat16 if out is None else out.dtype) if dtype is None else dtype
+    if str(dtype) not in _FLOATS:
+        raise TypeError("dtype must be float32 or bfloat16")
+    dev = b.packed.device
+    cols = a.cols if isinstance(a, Mxfp4) else a.shape[-1]
+    if cols != b.cols or (a.packed if isinstance(a, Mxfp4) else a).device != dev:
+        raise ValueError("a and b must have the same inner size and be on one GPU")
+    a = _as_mxfp4("a", a, stream)
+    out = _out_matrix("out", out, (a.rows, b.rows), dtype, dev)
+    _enqueue("dart_mxfp4_matmul", dev, stream, a.packed.data_ptr(), a.scales.data_ptr(), a.rows,
+             b.packed.data_ptr(), b.scales.data_ptr(), b.rows, b.cols, _FLOATS[str(dtype)],
+             out.data_ptr(), _ld(out))
+    return out
+
+
+def dart_lmhead_mxfp4_tok_stats(hidden, weight, target, inv_temp=1.0, logp=None, entropy=None,
+                                lse=None, workspace="auto", stream=None):
+    """(logp, entropy, lse) float32 [T] of softmax(inv_temp * hidden @ weight^T) for an Mxfp4 weight
+    [V, d] and hidden states [T, d] in Mxfp4, or in float32 or bfloat16 and quantised first: the
+    log-probs of a rollout policy whose head is kept in four bits, without materialising the logits.
+    ``workspace``: "auto" (allocated here) or a uint8 device tensor of
+    dart_lmhead_stats_workspace_bytes(T, V) bytes."""
+    torch = _torch()
+    _check_mxfp4("weight", weight)
+    dev = weight.packed.device
+    cols = hidden.cols if isinstance(hidden, Mxfp4) else hidden.shape[-1]
+    if cols != weight.cols or (hidden.packed if isinstance(hidden, Mxfp4) else hidden).device != dev:
+        raise ValueError("hidden and weight must have the same inner size d and be on one GPU")
+    T, V = hidden.rows if isinstance(hidden, Mxfp4) else hidden.shape[0], weight.rows
+    _check_vec("target", target, torch.int32, T, dev)
+    logp = torch.empty(T, dtype=torch.float32, device=dev) if logp is None else logp
+    entropy = torch.empty(T, dtype=torch.float32, device=dev) if entropy is None else entropy
+    lse = torch.empty(T, dtype=torch.float32, device=dev) if lse is None else lse
+    for n, v in (("logp", logp), ("entropy", entropy), ("lse", lse)):
+        _check_vec(n, v, torch.float32, T, dev)
+    if isinstance(workspace, str):
+        if workspace != "auto":
+            raise ValueError('workspace must be "auto" or a uint8 device tensor')
+        workspace = torch.empty(dart_lmhead_stats_workspace_bytes(T, V), dtype=torch.uint8,
+                                device=dev)
+        _used_on(stream, workspace)
+    if (not isinstance(workspace, torch.Tensor) or workspace.dtype != torch.uint8
+            or workspace.device != dev or not workspace.is_contiguous()):
+        raise ValueError("workspace must be a contiguous uint8 tensor on the device of the inputs")
+    hidden = _as_mxfp4("hidden", hidden, stream)
+    _enqueue("dart_lmhead_mxfp4_tok_stats", dev, stream, hidden.packed.data_ptr(),
+             hidden.scales.data_ptr(), T, weight.packed.data_ptr(), weight.scales.data_ptr(), V,
+             weight.cols, target.data_ptr(), float(inv_temp), logp.data_ptr(), entropy.data_ptr(),
+             lse.data_ptr(), workspace.data_ptr(), workspace.numel())
+    return logp, entropy, lse
 
 
 _UPDATE = ("logp", "entropy", "lse", "step_entropy", "step_mask", "n_kept_steps", "loss",
