@@ -559,6 +559,96 @@ size_t dart_lmhead_backward_split_workspace_bytes(int64_t T, int64_t d, int64_t 
                                                   uint32_t flags);
 
 /* ------------------------------------------------------------------------
+ * Supervised learning of the LM head: cross entropy and its gradient
+ * ------------------------------------------------------------------------ */
+
+/* Reduction of the tokens' losses: over the tokens with a label. */
+typedef enum { DART_XENT_MEAN = 0, DART_XENT_SUM = 1 } dart_xent_reduction_t;
+
+/* Cross-entropy configuration (host memory, read during the call). */
+typedef struct {
+    float label_smoothing; /* eps in [0, 1): the learnt distribution is 1 - eps on the target
+                              and eps / V on every entry */
+    float z_loss;          /* lambda >= 0, finite: weight of lse^2 */
+    int32_t reduction;     /* dart_xent_reduction_t */
+} dart_xent_config_t;
+
+/* The cross entropy of softmax(h W^T) with the targets, as a trainer learns
+ * from stored trajectories (Sec. 4.2's pool, a supervised start), without
+ * logits in memory. A row t has a label when 0 <= target[t] < V; with
+ * z = h W^T and lse_t = log sum_v exp(z_tv), N rows with a label:
+ *   tok_loss[t] = (1 - eps) (lse_t - z_{t,y}) + eps (lse_t - mean_v z_tv) + lambda lse_t^2
+ *   loss        = sum_t tok_loss[t] / N (mean) or the sum
+ * Rows without one (target < 0, such as the -100 of prompt tokens) have
+ * tok_loss 0 and no share in loss; N = 0 gives loss 0.
+ *   hidden, weight, d, ld_h, ld_w: as for dart_lmhead_tok_stats.
+ *   target:    [T] int32; values of V and above are a broken precondition
+ *              (reported under DART_CHECK=1, else taken as no label).
+ *   loss:      [1] float32 output (summed in float64 in a fixed order).
+ *   tok_loss:  [T] float32 output.   n_valid: [1] int32 output, N.
+ *   workspace: device memory of at least
+ *              dart_lmhead_xent_fwd_workspace_bytes(T, d, V) bytes, 16-byte
+ *              aligned, owned by the caller; contents on entry do not matter.
+ * A row's results do not depend on the other rows of the call. NaN or
+ * infinite logits show as NaN in the row's loss (and gradient).
+ * Errors: INVALID_ARG for a null pointer, sizes or alignments that
+ * dart_lmhead_tok_stats refuses, a value outside its range in config, or a
+ * workspace that is too small; UNSUPPORTED when ceil(T/256) * ceil(V/256)
+ * or T exceeds 8,388,607 or ld_h or ld_w 2^22; HIP when a launch fails. */
+dart_status_t dart_lmhead_xent_fwd(const void* hidden, int64_t T, int64_t d, int64_t ld_h,
+                                   const void* weight, int64_t V, int64_t ld_w,
+                                   const int32_t* target, const dart_xent_config_t* config,
+                                   float* loss, float* tok_loss, int32_t* n_valid, void* workspace,
+                                   size_t workspace_bytes, hipStream_t stream);
+
+/* dart_lmhead_xent_fwd and the gradients of loss with respect to the hidden
+ * states and the weight, in bfloat16:
+ *   dz_tv = ((1 + 2 lambda lse_t) p_tv - (1 - eps) [v = y_t] - eps / V) / N
+ *   dhidden = dz W [T, d],  dweight = dz^T h [V, d]
+ * (without the 1 / N for a sum; rows without a label are zeros of dz). The
+ * product h W^T is formed once, chunk_rows rows at a time: their exponentials
+ * are kept in the workspace and become dz there (bf16, as in
+ * dart_lmhead_dlogits), so that no more than chunk_rows x V of them ever
+ * exist. Rows without a label take no part in the products, whatever their hidden
+ * states hold (their count is read on the device: the call stays asynchronous and can be
+ * captured into a HIP graph, unless DART_CHECK=1); their rows of dhidden are 0.
+ *   dhidden, dweight: [T, ld_dh >= d], [V, ld_dw >= d] bfloat16 outputs, round to
+ *              nearest even, rounded once from fp32 sums; overwritten. One of
+ *              them may be NULL: it is then not formed.
+ *   chunk_rows: >= 1 (values above T are taken as T); with more than one chunk
+ *              dweight is summed in float32 in the workspace.
+ *   workspace: device memory of at least
+ *              dart_lmhead_xent_workspace_bytes(T, d, V, chunk_rows) bytes, 16-byte
+ *              aligned, owned by the caller; contents on entry do not matter.
+ * Other arguments, results and errors as dart_lmhead_xent_fwd (the losses up to the
+ * order of a row's sum over the vocabulary);
+ * INVALID_ARG also when both gradients are null, for ld_dh or ld_dw below d, or
+ * chunk_rows < 1; UNSUPPORTED also for V, ld_dh or ld_dw above 2^22. */
+dart_status_t dart_lmhead_xent_fwd_bwd(const void* hidden, int64_t T, int64_t d, int64_t ld_h,
+                                       const void* weight, int64_t V, int64_t ld_w,
+                                       const int32_t* target, const dart_xent_config_t* config,
+                                       float* loss, float* tok_loss, int32_t* n_valid,
+                                       void* dhidden, int64_t ld_dh, void* dweight, int64_t ld_dw,
+                                       int64_t chunk_rows, void* workspace, size_t workspace_bytes,
+                                       hipStream_t stream);
+
+/* Bytes of workspace of the two calls (0 for arguments outside
+ * [1, INT32_MAX]). The second is chunk_rows * ceil8(V) * 2 for the
+ * exponentials, chunk_rows * ceil(V/256) * 16 for partial sums, V * d * 4 where
+ * chunk_rows < T, T * (2 d + 8) for the labelled rows, and at most
+ * 64 MiB for dhidden's sum in parts where T and d are multiples of 256. Host only. */
+size_t dart_lmhead_xent_fwd_workspace_bytes(int64_t T, int64_t d, int64_t V);
+size_t dart_lmhead_xent_workspace_bytes(int64_t T, int64_t d, int64_t V, int64_t chunk_rows);
+
+/* x *= factor[0] for x [rows, ld >= cols] bf16 or fp32 (each product rounded once), factor a
+ * float32 in device memory: the incoming gradient of a loss whose gradients were formed with it.
+ * Where the factor is 1, x is neither read nor written. Errors: INVALID_ARG for a
+ * null or misaligned pointer, a size outside [1, INT32_MAX], ld < cols or an unknown dtype; HIP
+ * when the launch fails. */
+dart_status_t dart_grad_scale(void* x, dart_dtype_t dtype, int64_t rows, int64_t cols, int64_t ld,
+                              const float* factor, hipStream_t stream);
+
+/* ------------------------------------------------------------------------
  * The LM head in four bits (MXFP4)
  * ------------------------------------------------------------------------ */
 

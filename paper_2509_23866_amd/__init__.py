@@ -37,6 +37,7 @@ DART_BF16 = 1
 DART_KL = {"none": 0, "k1": 1, "k2": 2, "k3": 3}
 DART_AGG = {"token_mean": 0, "token_mean_all": 1, "step_mean": 2}
 DART_RATIO = {"token": 0, "step_geomean": 1, "step_product": 2}
+DART_XENT = {"mean": 0, "sum": 1}
 DART_GRAD_SKIP_ZERO_ROWS = 1
 DART_LMHEAD_SKIP_ZERO_ROWS = 1
 DART_LMHEAD_BF16_GRADS = 4
@@ -51,6 +52,8 @@ EXPORTED = ("dart_tok_stats", "dart_step_select", "dart_tis_loss_fwd_bwd", "dart
             "dart_lmhead_backward", "dart_lmhead_backward_workspace_bytes",
             "dart_lmhead_backward_ex", "dart_lmhead_backward_ex_workspace_bytes",
             "dart_lmhead_backward_split_workspace_bytes",
+            "dart_lmhead_xent_fwd", "dart_lmhead_xent_fwd_workspace_bytes",
+            "dart_lmhead_xent_fwd_bwd", "dart_lmhead_xent_workspace_bytes", "dart_grad_scale",
             "dart_mxfp4_packed_bytes", "dart_mxfp4_scales_bytes", "dart_mxfp4_quantize",
             "dart_mxfp4_dequantize", "dart_mxfp4_matmul", "dart_lmhead_mxfp4_tok_stats",
             "dart_kept_steps",
@@ -63,6 +66,13 @@ class dart_loss_config_t(ctypes.Structure):
     _fields_ = [("eps_low", ctypes.c_float), ("eps_high", ctypes.c_float), ("C", ctypes.c_float),
                 ("kl", ctypes.c_int32), ("beta", ctypes.c_float), ("aggregation", ctypes.c_int32),
                 ("ratio", ctypes.c_int32)]
+
+
+class dart_xent_config_t(ctypes.Structure):
+    """Mirror of the C struct dart_xent_config_t."""
+
+    _fields_ = [("label_smoothing", ctypes.c_float), ("z_loss", ctypes.c_float),
+                ("reduction", ctypes.c_int32)]
 
 
 class DartError(RuntimeError):
@@ -160,6 +170,20 @@ def load_library():
         lib.dart_lmhead_backward_split_workspace_bytes.restype = ctypes.c_size_t
         lib.dart_lmhead_backward_split_workspace_bytes.argtypes = [_I64, _I64, _I64, _I64, _I64,
                                                                    ctypes.c_uint32]
+        lib.dart_lmhead_xent_fwd.restype = ctypes.c_int
+        lib.dart_lmhead_xent_fwd.argtypes = [_P, _I64, _I64, _I64, _P, _I64, _I64, _P,
+                                             ctypes.POINTER(dart_xent_config_t), _P, _P, _P, _P,
+                                             ctypes.c_size_t, _P]
+        lib.dart_lmhead_xent_fwd_workspace_bytes.restype = ctypes.c_size_t
+        lib.dart_lmhead_xent_fwd_workspace_bytes.argtypes = [_I64, _I64, _I64]
+        lib.dart_lmhead_xent_fwd_bwd.restype = ctypes.c_int
+        lib.dart_lmhead_xent_fwd_bwd.argtypes = [_P, _I64, _I64, _I64, _P, _I64, _I64, _P,
+                                                 ctypes.POINTER(dart_xent_config_t), _P, _P, _P,
+                                                 _P, _I64, _P, _I64, _I64, _P, ctypes.c_size_t, _P]
+        lib.dart_lmhead_xent_workspace_bytes.restype = ctypes.c_size_t
+        lib.dart_lmhead_xent_workspace_bytes.argtypes = [_I64, _I64, _I64, _I64]
+        lib.dart_grad_scale.restype = ctypes.c_int
+        lib.dart_grad_scale.argtypes = [_P, ctypes.c_int, _I64, _I64, _I64, _P, _P]
         lib.dart_mxfp4_packed_bytes.restype = ctypes.c_size_t
         lib.dart_mxfp4_packed_bytes.argtypes = [_I64, _I64]
         lib.dart_mxfp4_scales_bytes.restype = ctypes.c_size_t
@@ -942,6 +966,125 @@ def _ld(t):
     return t.stride(0) if t.shape[0] > 1 else t.shape[1]
 
 
+def _byte_workspace(workspace, nbytes, device, stream):
+    """``workspace``, or for "auto" a new uint8 tensor of nbytes."""
+    torch = _torch()
+    if isinstance(workspace, str):
+        if workspace != "auto":
+            raise ValueError('workspace must be "auto" or a uint8 device tensor')
+        workspace = torch.empty(nbytes, dtype=torch.uint8, device=device)
+        _used_on(stream, workspace)
+    if (not isinstance(workspace, torch.Tensor) or workspace.dtype != torch.uint8
+            or workspace.device != device or not workspace.is_contiguous()):
+        raise ValueError("workspace must be a contiguous uint8 tensor on the device of the inputs")
+    return workspace
+
+
+def dart_lmhead_xent_fwd_workspace_bytes(T: int, d: int, V: int) -> int:
+    return int(load_library().dart_lmhead_xent_fwd_workspace_bytes(int(T), int(d), int(V)))
+
+
+def dart_lmhead_xent_workspace_bytes(T: int, d: int, V: int, chunk_rows: int) -> int:
+    return int(load_library().dart_lmhead_xent_workspace_bytes(int(T), int(d), int(V),
+                                                               int(chunk_rows)))
+
+
+def lmhead_xent_plan(T: int, V: int, budget_bytes: int = 2 << 30) -> int:
+    """chunk_rows for dart_lmhead_xent_fwd_bwd: all rows where their exponentials fit
+    budget_bytes, else as many whole tiles of 256 as do, the chunks of one size: each chunk reads
+    and rewrites the [V, d] sum of dweight."""
+    T, V = int(T), int(V)
+    most = max(budget_bytes // (2 * ((V + 7) // 8 * 8)), 256)
+    if T <= most:
+        return T
+    most = most // 256 * 256
+    chunks = -(-T // most)
+    return min(most, -(-T // chunks // 256) * 256)
+
+
+def _xent_inputs(hidden, weight, target, label_smoothing, z_loss, reduction):
+    torch = _torch()
+    _matrix_bf16("hidden", hidden)
+    dev = hidden.device
+    _matrix_bf16("weight", weight, dev)
+    T, d = hidden.shape
+    if weight.shape[1] != d:
+        raise ValueError("hidden and weight must have the same inner size d")
+    _check_vec("target", target, torch.int32, T, dev)
+    if reduction not in DART_XENT:
+        raise ValueError(f"reduction must be one of {sorted(DART_XENT)}")
+    config = dart_xent_config_t(float(label_smoothing), float(z_loss), DART_XENT[reduction])
+    return dev, T, d, weight.shape[0], config
+
+
+def dart_lmhead_xent_fwd(hidden, weight, target, label_smoothing=0.0, z_loss=0.0, reduction="mean",
+                         workspace="auto", stream=None):
+    """(loss float32 [1], tok_loss float32 [T], n_valid int32 [1]): the cross entropy of
+    softmax(hidden @ weight^T) with the targets, without materialising the logits; hidden [T, d] and
+    weight [V, d] bfloat16 (d a multiple of 8), target int32 [T]. Rows whose target is negative
+    (-100, say) have a loss of 0 and do not count. Per row, with eps = label_smoothing:
+    (1 - eps) (lse - z_y) + eps (lse - mean z) + z_loss lse^2; ``reduction``: "mean" over the rows
+    that count, or "sum". ``workspace``: "auto" (allocated here) or a uint8 device tensor of
+    dart_lmhead_xent_fwd_workspace_bytes(T, d, V) bytes."""
+    torch = _torch()
+    dev, T, d, V, config = _xent_inputs(hidden, weight, target, label_smoothing, z_loss, reduction)
+    loss = torch.empty(1, dtype=torch.float32, device=dev)
+    tok = torch.empty(T, dtype=torch.float32, device=dev)
+    n = torch.empty(1, dtype=torch.int32, device=dev)
+    workspace = _byte_workspace(workspace, dart_lmhead_xent_fwd_workspace_bytes(T, d, V), dev, stream)
+    _enqueue("dart_lmhead_xent_fwd", dev, stream, hidden.data_ptr(), T, d, _ld(hidden),
+             weight.data_ptr(), V, _ld(weight), target.data_ptr(), ctypes.byref(config),
+             loss.data_ptr(), tok.data_ptr(), n.data_ptr(), workspace.data_ptr(), workspace.numel())
+    return loss, tok, n
+
+
+def dart_lmhead_xent_fwd_bwd(hidden, weight, target, label_smoothing=0.0, z_loss=0.0,
+                             reduction="mean", chunk_rows=None, dhidden=None, dweight=None,
+                             want=(True, True), workspace="auto", stream=None):
+    """dart_lmhead_xent_fwd's (loss, tok_loss, n_valid) and the loss's gradients (dhidden [T, d],
+    dweight [V, d]) in bfloat16, the logits formed once: chunk_rows rows of their exponentials at a
+    time are kept in the workspace (default: lmhead_xent_plan's). ``want`` says which gradients to
+    form (None is returned for the other). ``workspace``: "auto" (allocated here) or a uint8 device
+    tensor of dart_lmhead_xent_workspace_bytes(T, d, V, chunk_rows) bytes."""
+    torch = _torch()
+    dev, T, d, V, config = _xent_inputs(hidden, weight, target, label_smoothing, z_loss, reduction)
+    want_h, want_w = want
+    if not (want_h or want_w):
+        raise ValueError("want at least one gradient")
+    bf16 = torch.bfloat16
+    chunk_rows = lmhead_xent_plan(T, V) if chunk_rows is None else max(1, min(int(chunk_rows), T))
+    dhidden = _out_matrix("dhidden", dhidden, (T, d), bf16, dev) if want_h else None
+    dweight = _out_matrix("dweight", dweight, (V, d), bf16, dev) if want_w else None
+    loss = torch.empty(1, dtype=torch.float32, device=dev)
+    tok = torch.empty(T, dtype=torch.float32, device=dev)
+    n = torch.empty(1, dtype=torch.int32, device=dev)
+    workspace = _byte_workspace(workspace, dart_lmhead_xent_workspace_bytes(T, d, V, chunk_rows),
+                                dev, stream)
+    _enqueue("dart_lmhead_xent_fwd_bwd", dev, stream, hidden.data_ptr(), T, d, _ld(hidden),
+             weight.data_ptr(), V, _ld(weight), target.data_ptr(), ctypes.byref(config),
+             loss.data_ptr(), tok.data_ptr(), n.data_ptr(), _ptr(dhidden),
+             _ld(dhidden) if want_h else 0, _ptr(dweight), _ld(dweight) if want_w else 0, chunk_rows,
+             workspace.data_ptr(), workspace.numel())
+    return loss, tok, n, dhidden, dweight
+
+
+def dart_grad_scale(x, factor, stream=None):
+    """x *= factor in place for a 2-D bfloat16 or float32 tensor with contiguous rows and a float32
+    scalar on the same GPU; where the factor is 1, x is not touched. Returns x."""
+    torch = _torch()
+    if not isinstance(x, torch.Tensor) or str(x.dtype) not in _FLOATS or x.dim() != 2:
+        raise TypeError("x must be a 2-D float32 or bfloat16 tensor")
+    if not x.is_cuda or x.numel() == 0:
+        raise ValueError("x must be on a GPU and not empty")
+    _out_matrix("x", x, tuple(x.shape), x.dtype, x.device)
+    if (not isinstance(factor, torch.Tensor) or factor.dtype != torch.float32
+            or factor.device != x.device or factor.numel() != 1):
+        raise ValueError(f"factor must be a float32 tensor of one element on {x.device}")
+    _enqueue("dart_grad_scale", x.device, stream, x.data_ptr(), _FLOATS[str(x.dtype)], x.shape[0],
+             x.shape[1], _ld(x), factor.data_ptr())
+    return x
+
+
 _FLOATS = {"torch.float32": DART_F32, "torch.bfloat16": DART_BF16}
 
 
@@ -1069,15 +1212,7 @@ def dart_lmhead_mxfp4_tok_stats(hidden, weight, target, inv_temp=1.0, logp=None,
     lse = torch.empty(T, dtype=torch.float32, device=dev) if lse is None else lse
     for n, v in (("logp", logp), ("entropy", entropy), ("lse", lse)):
         _check_vec(n, v, torch.float32, T, dev)
-    if isinstance(workspace, str):
-        if workspace != "auto":
-            raise ValueError('workspace must be "auto" or a uint8 device tensor')
-        workspace = torch.empty(dart_lmhead_stats_workspace_bytes(T, V), dtype=torch.uint8,
-                                device=dev)
-        _used_on(stream, workspace)
-    if (not isinstance(workspace, torch.Tensor) or workspace.dtype != torch.uint8
-            or workspace.device != dev or not workspace.is_contiguous()):
-        raise ValueError("workspace must be a contiguous uint8 tensor on the device of the inputs")
+    workspace = _byte_workspace(workspace, dart_lmhead_stats_workspace_bytes(T, V), dev, stream)
     hidden = _as_mxfp4("hidden", hidden, stream)
     _enqueue("dart_lmhead_mxfp4_tok_stats", dev, stream, hidden.packed.data_ptr(),
              hidden.scales.data_ptr(), T, weight.packed.data_ptr(), weight.scales.data_ptr(), V,

@@ -9,7 +9,8 @@ import sysconfig
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
-SRCS = [os.path.join(HERE, "csrc", n) for n in ("dart.hip", "lmhead.hip", "mxfp4.hip", "check.hip")]
+SRCS = [os.path.join(HERE, "csrc", n) for n in ("dart.hip", "lmhead.hip", "xent.hip", "mxfp4.hip",
+                                                     "check.hip")]
 LIB = os.path.join(HERE, "libdart.so")
 NATIVE_SRC = os.path.join(HERE, "csrc", "binding.cpp")
 NATIVE = os.path.join(HERE, "_native.so")

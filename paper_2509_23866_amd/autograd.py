@@ -19,6 +19,13 @@ only marshal tensors and scale the [T] coefficient.
 Both take inv_temp (default 1, the paper's value): the policy is then
 softmax(inv_temp z), as for dart_tok_stats_ex and dart_tis_grad_ex.
 
+    loss = dart_lmhead_xent_loss(hidden, weight, target)
+    loss.backward()          # hidden.grad, weight.grad (bfloat16)
+
+is the supervised counterpart: the cross entropy of the LM head's inputs, whose
+gradients are formed with the loss (their coefficients are known then) and
+scaled by the incoming gradient in the backward.
+
 The LM-head backward writes its gradients in bfloat16 directly and, unless
 told otherwise, forms the dlogits in the blocks of rows x vocabulary entries
 that lmhead_backward_plan picks for a 512 MiB workspace.
@@ -26,7 +33,8 @@ that lmhead_backward_plan picks for a 512 MiB workspace.
 
 import torch
 
-from . import (DART_LMHEAD_BF16_GRADS, dart_lmhead_backward_ex, dart_lmhead_tok_stats_ex,
+from . import (DART_LMHEAD_BF16_GRADS, dart_grad_scale, dart_lmhead_backward_ex,
+               dart_lmhead_tok_stats_ex, dart_lmhead_xent_fwd, dart_lmhead_xent_fwd_bwd,
                dart_select_tis_loss_fwd, dart_tis_grad, dart_tok_stats, lmhead_backward_plan)
 
 
@@ -120,3 +128,70 @@ def dart_lmhead_policy_loss(hidden, weight, target, logp_old, logp_rollout, adv,
     return DartLmHeadPolicyLoss.apply(hidden, weight, target, logp_old, logp_rollout, adv,
                                       step_offsets, rho, eps_low, eps_high, C, chunk_rows,
                                       chunk_cols, flags, float(inv_temp))
+
+
+class DartLmHeadXent(torch.autograd.Function):
+    """Scalar cross entropy (float32) of hidden [T, d] and weight [V, d] (bfloat16) through
+    logits h W^T that are never written to memory; the gradients that are wanted are formed
+    with it."""
+
+    @staticmethod
+    def forward(ctx, hidden, weight, target, options, want):
+        hidden, weight = hidden.detach(), weight.detach()
+        if not any(want):
+            return dart_lmhead_xent_fwd(hidden, weight, target, *options[:3])[0].reshape(())
+        loss, _, _, *grads = dart_lmhead_xent_fwd_bwd(hidden, weight, target, *options, want=want)
+        ctx.options, ctx.want, ctx.grads = options, want, grads
+        ctx.save_for_backward(hidden, weight, target)
+        return loss.reshape(())
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, grad):
+        hidden, weight, target = ctx.saved_tensors
+        # the gradients are handed over; a second backward of a retained graph forms them again
+        grads, ctx.grads = ctx.grads, None
+        if grads is None:
+            _, _, _, *grads = dart_lmhead_xent_fwd_bwd(hidden, weight, target, *ctx.options,
+                                                       want=ctx.want)
+        factor = grad.reshape(1).float()
+        return tuple(None if g is None else dart_grad_scale(g, factor) for g in grads) + (None,) * 3
+
+
+_LEAF_STREAM = "dart_lmhead_xent_loss stream"
+
+
+def _refuse_mixed_capture(leaves):
+    """torch's engine ends a backward pass by having the stream on which a leaf's gradient
+    accumulator was made wait for it. That node lives as long as any graph of the leaf: under HIP
+    graph capture, one that an eager loss made on another stream would pull that stream into the
+    capture, which ends the process. So a loss leaves its stream with the node (_mark_leaves), and
+    under capture a node with another's is refused."""
+    for leaf in leaves:
+        made_on = torch.autograd.graph.get_gradient_edge(leaf).node.metadata.get(_LEAF_STREAM)
+        if made_on not in (None, torch.cuda.current_stream(leaf.device).cuda_stream):
+            raise RuntimeError("a loss of this leaf from another stream is still alive: release it "
+                               "before capturing a backward pass of the leaf")
+
+
+def _mark_leaves(leaves):
+    """Once the loss's graph holds the leaves' accumulators."""
+    for leaf in leaves:
+        torch.autograd.graph.get_gradient_edge(leaf).node.metadata.setdefault(
+            _LEAF_STREAM, torch.cuda.current_stream(leaf.device).cuda_stream)
+
+
+def dart_lmhead_xent_loss(hidden, weight, target, label_smoothing=0.0, z_loss=0.0,
+                          reduction="mean", chunk_rows=None):
+    """Differentiable cross entropy of the LM head's inputs (see the module docstring);
+    arguments as for dart_lmhead_xent_fwd_bwd. Rows with a negative target do not count. Under
+    HIP graph capture no eager loss of the same leaves may be alive (a RuntimeError where it is one
+    of these; for others' graphs torch does not say)."""
+    want = tuple(torch.is_grad_enabled() and t.requires_grad for t in (hidden, weight))
+    leaves = [t for t, wanted in zip((hidden, weight), want) if wanted and t.is_leaf and t.is_cuda]
+    if leaves and torch.cuda.is_current_stream_capturing():
+        _refuse_mixed_capture(leaves)
+    loss = DartLmHeadXent.apply(hidden, weight, target,
+                                (float(label_smoothing), float(z_loss), reduction, chunk_rows), want)
+    _mark_leaves(leaves)
+    return loss

@@ -20,11 +20,12 @@ constexpr int kCheckThreads = 256;
 constexpr int64_t kCheckMaxBlocks = 1024;
 
 __global__ void __launch_bounds__(kCheckThreads)
-check_ids_kernel(const int32_t* __restrict__ v, int64_t n, int64_t bound, unsigned int* flag) {
+check_ids_kernel(const int32_t* __restrict__ v, int64_t n, int64_t least, int64_t bound,
+                 unsigned int* flag) {
     for (int64_t i = blockIdx.x * (int64_t)kCheckThreads + threadIdx.x; i < n;
          i += (int64_t)gridDim.x * kCheckThreads) {
         const int64_t x = v[i];
-        if (x < 0 || x >= bound) *flag = 1u;
+        if (x < least || x >= bound) *flag = 1u;
     }
 }
 
@@ -82,9 +83,11 @@ dart_status_t run(hipStream_t stream, std::initializer_list<Item> items) {
         if (!it.ptr) continue;
         switch (it.kind) {
             case Item::Ids:
+            case Item::Labels:
                 if (it.n > 0)
                     hipLaunchKernelGGL(check_ids_kernel, dim3(blocks_for(it.n)), dim3(kCheckThreads),
-                                       0, stream, static_cast<const int32_t*>(it.ptr), it.n, it.bound,
+                                       0, stream, static_cast<const int32_t*>(it.ptr), it.n,
+                                       it.kind == Item::Ids ? int64_t(0) : INT64_MIN, it.bound,
                                        flags + 0);
                 break;
             case Item::Offsets:

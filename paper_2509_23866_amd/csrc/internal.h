@@ -57,8 +57,9 @@ namespace dart_check {
 //   Ids:     n int32 values, each in [0, bound)
 //   Offsets: n + 1 int32 values, 0 = v[0] < v[1] < ... < v[n] = bound
 //   Mask:    n uint8 values, each 0 or 1
+//   Labels:  n int32 values, each below bound
 struct Item {
-    enum Kind { Ids, Offsets, Mask } kind;
+    enum Kind { Ids, Offsets, Mask, Labels } kind;
     const void* ptr;
     int64_t n;
     int64_t bound;
@@ -75,5 +76,56 @@ __attribute__((visibility("hidden"))) dart_status_t run(hipStream_t stream,
                                                         std::initializer_list<Item> items);
 
 }  // namespace dart_check
+
+// What the LM head's gradient calls share (lmhead.hip).
+namespace lmhead {
+
+// A gradient output: row-major, fp32 or bf16.
+struct Grad {
+    void* p;
+    int64_t ld;
+    bool bf16;
+    void* row(int64_t r) const {
+        return static_cast<char*>(p) + r * ld * (bf16 ? 2 : 4);
+    }
+};
+
+// One block's dh[rows, d] (+)= dz[rows, cols] W[cols, d] and
+// dW[cols, d] (+)= dz[rows, cols]^T h[rows, d], in one launch. A bf16 output
+// is never added to (sums over blocks go through fp32). With ksplit > 1 dh_out is
+// ksplit fp32 matrices part_stride elements apart, which each get their part of
+// the sum. With dh_map row i of dh goes to row dh_map[i] of dh_out. With dyn_rows,
+// the block's rows are at most *dyn_rows - dyn_base (read on the device).
+// A null dh_out.p or dw_out.p leaves that product out; scale (device memory, may be
+// null) is a factor of both.
+__attribute__((visibility("hidden"))) dart_status_t launch_bwd_gemms(
+    const uint16_t* dz, int64_t ld_dz, int64_t rows, int64_t cols, const uint16_t* w, int64_t ld_w,
+    const uint16_t* h, int64_t ld_h, int64_t d, const Grad& dh_out, bool dh_acc, int64_t ksplit,
+    int64_t part_stride, const Grad& dw_out, bool dw_acc, hipStream_t stream, const int32_t* dh_map,
+    const int32_t* dyn_rows, int64_t dyn_base, const float* scale);
+
+// Parts of a block's dh sum. dh has rows / 256 x d / 256 tiles, each a sum over
+// the block's whole vocabulary, and one launch holds them and dW's tiles, the
+// same work in many short sums: while dh's tiles fill less than half of the
+// compute units the launch waits for them (at 1000 rows, d = 3584, V = 152064:
+// 56 tiles of 2376 slices, 3.62 ms; in 2, 4 or 9 parts 2.10, 1.95 or 2.02 ms, adding
+// them up 7, 17 or 37 us more). So that at least half
+// and at most all of the units have a part, none shorter than kMinPartSlices.
+__attribute__((visibility("hidden"))) int64_t dh_parts(int64_t rows, int64_t d, int64_t cols);
+
+// The ksplit parts of dh (each [rows, d] fp32, part_stride elements apart) added up in
+// part order into out: row r to row r, or (map, its first entry that of row 0) to row
+// map[r]; with dyn_rows rows below *dyn_rows - dyn_base.
+__attribute__((visibility("hidden"))) void launch_sum_parts(
+    const float* parts, int64_t ksplit, int64_t part_stride, int64_t rows, int64_t d,
+    const int32_t* map, const Grad& out, const int32_t* dyn_rows, int64_t dyn_base,
+    hipStream_t stream);
+
+// dst [rows, cols] in bf16 from fp32 rows of cols elements.
+__attribute__((visibility("hidden"))) void launch_to_bf16(const float* src, int64_t rows,
+                                                          int64_t cols, const Grad& dst,
+                                                          hipStream_t stream);
+
+}  // namespace lmhead
 
 #pragma GCC visibility pop

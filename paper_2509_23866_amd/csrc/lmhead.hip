@@ -448,6 +448,8 @@ struct BwdGemm {
     // the sum over k in ksplit parts of kper (a multiple of BK), part i written
     // to out + i * part_stride elements
     int64_t ksplit, kper, part_stride;
+    // optional: a factor of the result (device memory)
+    const float* scale;
 };
 
 // Output modes of a backward GEMM: fp32 written, fp32 added to, bf16 written.
@@ -501,6 +503,15 @@ __device__ __forceinline__ void bwd_gemm_tile(const BwdGemm& g, int64_t b, typen
     const int64_t m0 = mt * C::BM, n0 = nt * C::BN;
     f32x16 acc[C::TM][C::TN];
     gemm_tile_bwd<C, A_KMAJ>(g.A, g.lda, g.B, g.ldb, M, N, kbeg, K, m0, n0, sm, acc);
+    if (g.scale) {
+        const float f = *g.scale;
+#pragma unroll
+        for (int i = 0; i < C::TM; ++i)
+#pragma unroll
+            for (int j = 0; j < C::TN; ++j)
+#pragma unroll
+                for (int v = 0; v < 16; ++v) acc[i][j][v] *= f;
+    }
 
     // Pieces of 32 rows x 64 columns through the wave's own part of the LDS, without
     // barriers, as in lmhead_dlogits_tile: a row's piece leaves as 16-byte vectors (vec),
@@ -821,6 +832,8 @@ size_t dart_lmhead_backward_workspace_bytes(int64_t chunk_rows, int64_t V) {
 
 namespace {
 
+using lmhead::Grad;
+
 constexpr uint32_t kBackwardFlags = DART_LMHEAD_SKIP_ZERO_ROWS | DART_LMHEAD_BF16_GRADS;
 
 int64_t ceil8(int64_t x) { return (x + 7) / 8 * 8; }
@@ -855,22 +868,6 @@ struct BackwardPlan {
 bool leaves_zero_rows_out(int64_t T, int64_t d, int64_t V) {
     return T >= 256 && (double)T * (double)V * (double)d >= 1e11 &&
            (double)T * (double)(6 * d + 20) <= double(128 << 20);
-}
-
-// Parts of a block's dh sum. dh has rows / 256 x d / 256 tiles, each a sum over
-// the block's whole vocabulary, and one launch holds them and dW's tiles, the
-// same work in many short sums: while dh's tiles fill less than half of the
-// compute units the launch waits for them (at 1000 rows, d = 3584, V = 152064:
-// 56 tiles of 2376 slices, 3.62 ms; in 2, 4 or 9 parts 2.10, 1.95 or 2.02 ms, adding
-// them up 7, 17 or 37 us more). So that at least half
-// and at most all of the units have a part, none shorter than kMinPartSlices.
-constexpr int64_t kMinPartSlices = 32;
-int64_t dh_parts(int64_t rows, int64_t d, int64_t cols) {
-    const int64_t tiles =
-        ((rows + LmCfg::BM - 1) / LmCfg::BM) * ((d + LmCfg::BN - 1) / LmCfg::BN);
-    const int64_t by_units = kUnits / tiles, by_k = cols / (LmCfg::BK * kMinPartSlices);
-    const int64_t n = by_units < by_k ? by_units : by_k;
-    return n > 1 ? n : 1;
 }
 
 // total = 0 when the sizes do not fit the address arithmetic.
@@ -909,23 +906,13 @@ BackwardPlan plan_backward(int64_t T, int64_t d, int64_t V, int64_t chunk_rows,
     };
     if (P.skip) take_rows();
     P.total = end;
-    P.ksplit = dh_parts(P.rows, d, P.cols);
+    P.ksplit = lmhead::dh_parts(P.rows, d, P.cols);
     P.compact = !P.skip && leaves_zero_rows_out(T, d, V);
     if (P.compact) take_rows();
     if (P.ksplit > 1) P.parts = take((size_t)P.ksplit * (size_t)P.rows * (size_t)d * 4);
     P.split_total = end;
     return P;
 }
-
-// A gradient output: row-major, fp32 or bf16.
-struct Grad {
-    void* p;
-    int64_t ld;
-    bool bf16;
-    void* row(int64_t r) const {
-        return static_cast<char*>(p) + r * ld * (bf16 ? 2 : 4);
-    }
-};
 
 // The GEMM description of one backward output (out.p at the block's first
 // row); mode: kOutF32, kOutF32Acc or kOutBf16.
@@ -940,6 +927,7 @@ BwdGemm make_bwd_gemm(const uint16_t* A, int64_t lda, const uint16_t* B, int64_t
     g.nnt = (N + LmCfg::BN - 1) / LmCfg::BN;
     g.dyn = nullptr, g.dyn_base = 0, g.dyn_m = g.dyn_k = false;
     g.map = nullptr, g.ksplit = 1, g.kper = K, g.part_stride = 0;
+    g.scale = nullptr;
     return g;
 }
 
@@ -962,18 +950,16 @@ void launch_bwd_gemms_dw(int dw_mode, const BwdGemm& dh, const BwdGemm& dw, int6
     else launch_bwd_gemms_t<DH, kOutBf16>(dh, dw, n_dh, blocks, stream);
 }
 
-// One block's dh[rows, d] (+)= dz[rows, cols] W[cols, d] and
-// dW[cols, d] (+)= dz[rows, cols]^T h[rows, d], in one launch. A bf16 output
-// is never added to (sums over blocks go through fp32). With ksplit > 1 dh_out is
-// ksplit fp32 matrices part_stride elements apart, which each get their part of
-// the sum. With dh_map row i of dh goes to row dh_map[i] of dh_out. With dyn_rows,
-// the block's rows are at most *dyn_rows - dyn_base (read on the device).
-dart_status_t launch_bwd_gemms(const uint16_t* dz, int64_t ld_dz, int64_t rows, int64_t cols,
-                               const uint16_t* w, int64_t ld_w, const uint16_t* h, int64_t ld_h,
-                               int64_t d, const Grad& dh_out, bool dh_acc, int64_t ksplit,
-                               int64_t part_stride, const Grad& dw_out, bool dw_acc,
-                               hipStream_t stream, const int32_t* dh_map, const int32_t* dyn_rows,
-                               int64_t dyn_base) {
+constexpr int64_t kMinPartSlices = 32;
+
+}  // namespace
+
+dart_status_t lmhead::launch_bwd_gemms(const uint16_t* dz, int64_t ld_dz, int64_t rows, int64_t cols,
+                                       const uint16_t* w, int64_t ld_w, const uint16_t* h, int64_t ld_h,
+                                       int64_t d, const Grad& dh_out, bool dh_acc, int64_t ksplit,
+                                       int64_t part_stride, const Grad& dw_out, bool dw_acc,
+                                       hipStream_t stream, const int32_t* dh_map, const int32_t* dyn_rows,
+                                       int64_t dyn_base, const float* scale) {
     if ((dh_out.bf16 && dh_acc) || (dw_out.bf16 && dw_acc)) return DART_ERR_INVALID_ARG;
     if (ld_dz > kMaxLd || ld_w > kMaxLd || ld_h > kMaxLd || dh_out.ld > kMaxLd ||
         dw_out.ld > kMaxLd)
@@ -985,13 +971,15 @@ dart_status_t launch_bwd_gemms(const uint16_t* dz, int64_t ld_dz, int64_t rows, 
     dh.dyn_base = dw.dyn_base = dyn_base;
     dh.dyn_m = dw.dyn_k = dyn_rows != nullptr;
     dh.map = dh_map;
+    dh.scale = dw.scale = scale;
     if (ksplit > 1) {
         const int64_t nk = (cols + LmCfg::BK - 1) / LmCfg::BK;
         dh.ksplit = ksplit, dh.kper = (nk + ksplit - 1) / ksplit * LmCfg::BK;
         dh.part_stride = part_stride;
     }
-    const int64_t n_dh = (dh.nmt * dh.nnt * ksplit + 7) / 8 * 8;
-    const int64_t blocks = n_dh + dw.nmt * dw.nnt;
+    const int64_t n_dh = dh_out.p ? (dh.nmt * dh.nnt * ksplit + 7) / 8 * 8 : 0;
+    const int64_t blocks = n_dh + (dw_out.p ? dw.nmt * dw.nnt : 0);
+    if (blocks == 0) return DART_OK;
     if (!grid_fits(blocks, LmCfg::THREADS)) return DART_ERR_UNSUPPORTED;
     const int dhm = out_mode(dh_out, dh_acc), dwm = out_mode(dw_out, dw_acc);
     if (dhm == kOutF32) launch_bwd_gemms_dw<kOutF32>(dwm, dh, dw, n_dh, blocks, stream);
@@ -1000,12 +988,37 @@ dart_status_t launch_bwd_gemms(const uint16_t* dz, int64_t ld_dz, int64_t rows, 
     return hipGetLastError() == hipSuccess ? DART_OK : DART_ERR_HIP;
 }
 
-void launch_to_bf16(const float* src, int64_t rows, int64_t cols, const Grad& dst,
+void lmhead::launch_to_bf16(const float* src, int64_t rows, int64_t cols, const Grad& dst,
                     hipStream_t stream) {
     const unsigned blocks = (unsigned)(rows < kRowBlocks ? rows : kRowBlocks);
     hipLaunchKernelGGL(to_bf16_kernel, dim3(blocks), dim3(256), 0, stream, src, cols, rows, cols,
                        static_cast<uint16_t*>(dst.p), dst.ld);
 }
+
+void lmhead::launch_sum_parts(const float* parts, int64_t ksplit, int64_t part_stride, int64_t rows,
+                              int64_t d, const int32_t* map, const Grad& out,
+                              const int32_t* dyn_rows, int64_t dyn_base, hipStream_t stream) {
+    const int64_t blocks = (rows * d / 4 + 255) / 256;
+    const dim3 grid((unsigned)(blocks < kRowBlocks ? blocks : kRowBlocks));
+    if (out.bf16)
+        hipLaunchKernelGGL(sum_parts_kernel<uint16_t>, grid, dim3(256), 0, stream, parts, ksplit,
+                           part_stride, rows, d, map, static_cast<uint16_t*>(out.p), out.ld,
+                           dyn_rows, dyn_base);
+    else
+        hipLaunchKernelGGL(sum_parts_kernel<float>, grid, dim3(256), 0, stream, parts, ksplit,
+                           part_stride, rows, d, map, static_cast<float*>(out.p), out.ld, dyn_rows,
+                           dyn_base);
+}
+
+int64_t lmhead::dh_parts(int64_t rows, int64_t d, int64_t cols) {
+    const int64_t tiles =
+        ((rows + LmCfg::BM - 1) / LmCfg::BM) * ((d + LmCfg::BN - 1) / LmCfg::BN);
+    const int64_t by_units = kUnits / tiles, by_k = cols / (LmCfg::BK * kMinPartSlices);
+    const int64_t n = by_units < by_k ? by_units : by_k;
+    return n > 1 ? n : 1;
+}
+
+namespace {
 
 // The gradient pass over rows [0, T) of h in blocks of rows x vocabulary
 // entries: per block, its dlogits into dz (bf16), then the block's share of
@@ -1038,16 +1051,8 @@ dart_status_t backward_core(const uint16_t* h, int64_t T, int64_t d,
     const bool via_h = !parts && dh.bf16 && C < V, via_w = dw.bf16 && R < T;
     const bool put = map && !parts && !via_h;
     auto sum_parts = [&](const float* p, int64_t n, int64_t stride, int64_t r0, int64_t rows) {
-        const int64_t blocks = (rows * d / 4 + 255) / 256;
-        const dim3 grid((unsigned)(blocks < kRowBlocks ? blocks : kRowBlocks));
-        const int32_t* m = map ? map + r0 : nullptr;
-        void* out = map ? dh.p : dh.row(r0);
-        if (dh.bf16)
-            hipLaunchKernelGGL(sum_parts_kernel<uint16_t>, grid, dim3(256), 0, stream, p, n, stride,
-                               rows, d, m, static_cast<uint16_t*>(out), dh.ld, dyn_rows, r0);
-        else
-            hipLaunchKernelGGL(sum_parts_kernel<float>, grid, dim3(256), 0, stream, p, n, stride,
-                               rows, d, m, static_cast<float*>(out), dh.ld, dyn_rows, r0);
+        lmhead::launch_sum_parts(p, n, stride, rows, d, map ? map + r0 : nullptr,
+                                 map ? dh : Grad{dh.row(r0), dh.ld, dh.bf16}, dyn_rows, r0, stream);
     };
     const Grad sum_h = via_h ? Grad{acc_h, d, false} : dh;
     const Grad sum_w = via_w ? Grad{acc_w, d, false} : dw;
@@ -1061,12 +1066,12 @@ dart_status_t backward_core(const uint16_t* h, int64_t T, int64_t d,
                 launch_dlogits(hr, rows, d, ld_h, wc, cols, ld_w, target + r0, lse + r0,
                                logp + r0, coef + r0, scale, dz, ld_dz, c0, stream, dyn_rows, r0);
             if (st != DART_OK) return st;
-            const dart_status_t sg = launch_bwd_gemms(
+            const dart_status_t sg = lmhead::launch_bwd_gemms(
                 dz, ld_dz, rows, cols, wc, ld_w, hr, ld_h, d,
                 parts ? Grad{parts, d, false}
                       : Grad{put ? sum_h.p : sum_h.row(r0), sum_h.ld, sum_h.bf16},
                 c0 > 0, parts ? ksplit : 1, R * d, Grad{sum_w.row(c0), sum_w.ld, sum_w.bf16},
-                r0 > 0, stream, put ? map + r0 : nullptr, dyn_rows, r0);
+                r0 > 0, stream, put ? map + r0 : nullptr, dyn_rows, r0, nullptr);
             if (sg != DART_OK) return sg;
         }
         if (parts) sum_parts(parts, ksplit, R * d, r0, rows);
@@ -1074,8 +1079,8 @@ dart_status_t backward_core(const uint16_t* h, int64_t T, int64_t d,
     if (via_h && map)
         sum_parts(acc_h, 1, 0, 0, T);
     else if (via_h)
-        launch_to_bf16(acc_h, T, d, dh, stream);
-    if (via_w) launch_to_bf16(acc_w, V, d, dw, stream);
+        lmhead::launch_to_bf16(acc_h, T, d, dh, stream);
+    if (via_w) lmhead::launch_to_bf16(acc_w, V, d, dw, stream);
     return hipGetLastError() == hipSuccess ? DART_OK : DART_ERR_HIP;
 }
 

@@ -692,7 +692,7 @@ __device__ __forceinline__ void stats_of_tile(F&& tile, int64_t T, int64_t V,
 // then across lanes by a butterfly; the target logit is added last, as in
 // tok_stats_kernel: lse = M + log S, H = log S - W / S, and logp from
 // -log1p(s_rest / e_y) when the target dominates.
-__global__ void __launch_bounds__(kMergeWaves * 64)
+[[maybe_unused]] __global__ void __launch_bounds__(kMergeWaves * 64)
 lmhead_merge_kernel(const float4* __restrict__ part, const float* __restrict__ z_y, int64_t T,
                     int64_t nvt, int64_t V, const int32_t* __restrict__ target,
                     float* __restrict__ logp, float* __restrict__ entropy,

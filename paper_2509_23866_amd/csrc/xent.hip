@@ -1,0 +1,620 @@
+// libdart, supervised part: the cross entropy of the LM head and its gradient, straight
+// from the hidden states and the head's weight.
+//
+// For the rows t whose target y_t lies in [0, V), with z = h W^T and lse_t = log sum_v e^z_tv:
+//   l_t   = (1 - eps) (lse_t - z_ty) + eps (lse_t - mean_v z_tv) + lambda lse_t^2
+//   dl/dz = (1 + 2 lambda lse_t) p_tv - (1 - eps) [v = y_t] - eps / V
+// and 0 for the others. Forward alone: the tile of lmhead_stats_kernel reduced to (max,
+// normaliser, sum) per row and 256 columns, merged per row. With the gradient, rows are
+// taken a block at a time, and the product z is formed once:
+//   xent_tile_kernel  forms z tile by tile on the matrix cores, reduces each row's 256
+//                     columns to a triple, and keeps e = 2^15 e^(z - max) of them in fp16;
+//   xent_rows_kernel  merges a row's triples to lse, and turns its e in place into the
+//                     bf16 dz / (1 - eps), from which no logit is needed;
+//   the GEMMs of the LM head's backward (dh = dz W, dW = dz^T h), times (1 - eps) / N.
+// The rows with a label are gathered first, so that the others cost no product, and
+// whatever their hidden states hold (NaNs in the padding of a batch) reaches no result.
+// So three products of T V d instead of the four of a loss whose coefficients only a
+// second pass knows (dart_lmhead_backward): at T = 4096, V = 152064, d = 3584 the kept
+// exponentials cost a read and a write of 1.25 GB, the fourth product took 3.4 ms.
+// What is rounded: e to fp16 (2^-12 of its value down to 2^-29 of its tile's maximum, below
+// that 2^-40 of the maximum: little beside the bf16 that follows), dz to bf16 for the
+// matrix cores, as in dart_lmhead_dlogits. dz is kept divided by 1 - eps and not yet by N,
+// so that the target's element of an unsure row, the largest of all, is next to -1 and
+// loses nothing by its rounding.
+#include "lmhead_tile.h"
+
+namespace {
+
+using lmhead::Grad;
+
+constexpr float kLog2e = 1.4426950408889634f;
+// exponentials are kept times 2^kShift: fp16 holds up to 65504 and 2^-14 at full width
+constexpr int kShift = 15;
+constexpr int kUnitsPerTile = LmCfg::BN / kStatsUnit;
+
+__device__ __forceinline__ bool has_label(int32_t y, int64_t V) { return y >= 0 && y < V; }
+
+// Four adjacent columns as fp16.
+__device__ __forceinline__ u32x2 pack_half4(float a, float b, float c, float d) {
+    typedef _Float16 h4 __attribute__((ext_vector_type(4)));
+    const h4 v = {(_Float16)a, (_Float16)b, (_Float16)c, (_Float16)d};
+    return __builtin_bit_cast(u32x2, v);
+}
+
+// Partial results of a tile's rows, one per unit of 64 columns: maxima, normalisers, sums.
+struct Units {
+    float v[3][kUnitsPerTile][LmCfg::BM];
+};
+
+// Tile (m0, vt) of the logits: part[t * nvt + vt] = (max, sum of e^(z - max), sum of z, 0) of
+// row t over the tile's columns, the target's column in the sum of z alone; the workgroup
+// holding target[t] writes z_y[t]. With KEEP e [M, ld_e] receives 2^15 e^(z - max) in fp16 (0
+// in the target's column). Sums run in the order of lmhead_stats_kernel's, whatever the
+// tile's height, so that equal rows have equal results.
+template <class C, bool KEEP>
+__device__ __forceinline__ void xent_tile(const uint16_t* __restrict__ h, int64_t M, int64_t ldh,
+                                          const uint16_t* __restrict__ w, int64_t V, int64_t ldw,
+                                          int64_t d, const int32_t* __restrict__ target,
+                                          int64_t nvt, float4* __restrict__ part,
+                                          float* __restrict__ z_y, uint16_t* __restrict__ e,
+                                          int64_t ld_e, typename C::Smem& sm, Units& units,
+                                          int64_t m0, int64_t vt) {
+#pragma clang fp contract(off)  // the same roundings in every configuration
+    const int64_t n0 = vt * C::BN;
+    f32x16 acc[C::TM][C::TN];
+    gemm_tile<C>(h, M, ldh, w, V, ldw, d, m0, n0, sm, acc);
+
+    const int tid = threadIdx.x, lane = tid & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), half = lane >> 5;
+    const int wr = (wave / C::WN) * 32 + (lane & 31), wc = (wave % C::WN) * (C::BN / C::WN);
+    static_assert(C::TN % 2 == 0, "units of two 32-column blocks");
+#pragma unroll
+    for (int i = 0; i < C::TM; ++i) {
+        const int row = wr + i * C::RS;
+        const int64_t t = m0 + row;
+        const int64_t y = t < M ? (int64_t)target[t] : -1;
+#pragma unroll
+        for (int u = 0; u < C::TN / 2; ++u) {
+            const int64_t u0 = n0 + wc + u * kStatsUnit;
+            // the columns and the target within the unit, as in stats_of_tile
+            const int vlim = (int)max(min(V - u0, (int64_t)kStatsUnit), (int64_t)0);
+            const int64_t yrel = y - u0;
+            const int y64 = yrel >= 0 && yrel < vlim ? (int)yrel : -1;
+            float zs = 0.f;
+            const bool masked = vlim < kStatsUnit || (y64 >= 0 && ((y64 >> 2) & 1) == half);
+            if (masked) {
+                float zy = 0.f;
+                int vl = vlim - half * 4, yl = y64 - half * 4;
+                asm volatile("" : "+v"(vl), "+v"(yl));  // as in stats_of_tile
+#pragma unroll
+                for (int j = 0; j < 2; ++j)
+#pragma unroll
+                    for (int v = 0; v < 16; ++v) {
+                        const int col = j * 32 + (v >> 2) * 8 + (v & 3);
+                        const float x = acc[i][2 * u + j][v];
+                        const bool at_y = col == yl;
+                        zy = at_y ? x : zy;
+                        zs += col >= vl ? 0.f : x;
+                        acc[i][2 * u + j][v] = col >= vl || at_y ? -INFINITY : x;
+                    }
+                if (y64 >= 0 && ((y64 >> 2) & 1) == half) z_y[t] = zy;
+            } else {
+#pragma unroll
+                for (int j = 0; j < 2; ++j)
+#pragma unroll
+                    for (int v = 0; v < 16; ++v) zs += acc[i][2 * u + j][v];
+            }
+            float mx = -INFINITY;
+#pragma unroll
+            for (int j = 0; j < 2; ++j)
+#pragma unroll
+                for (int v = 0; v < 16; ++v) mx = fmaxf(mx, acc[i][2 * u + j][v]);
+            mx = fmaxf(mx, __shfl_xor(mx, 32));
+            zs += __shfl_xor(zs, 32);
+            if (half == 0) {
+                units.v[0][wc / kStatsUnit + u][row] = mx;
+                units.v[2][wc / kStatsUnit + u][row] = zs;
+            }
+        }
+    }
+    lds_ring_barrier();
+    constexpr int CPR = C::TN * 4, RPI = 64 / CPR;  // 16-byte chunks a row, rows a store
+#pragma unroll
+    for (int i = 0; i < C::TM; ++i) {
+        const int row = wr + i * C::RS;
+        float m = units.v[0][0][row];
+#pragma unroll
+        for (int k = 1; k < kUnitsPerTile; ++k) m = fmaxf(m, units.v[0][k][row]);
+        // nothing but the target: every exponential below is 0
+        const float ml = (m == -INFINITY ? 0.f : m * kLog2e) - (float)kShift;
+#pragma unroll
+        for (int u = 0; u < C::TN / 2; ++u) {
+            float s2[2];
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+                s2[j] = 0.f;
+#pragma unroll
+                for (int v = 0; v < 16; ++v) {
+                    const float x =
+                        __builtin_amdgcn_exp2f(fmaf(acc[i][2 * u + j][v], kLog2e, -ml));
+                    acc[i][2 * u + j][v] = x;
+                    s2[j] += x;
+                }
+            }
+            float s = s2[0] + s2[1];
+            s += __shfl_xor(s, 32);
+            if (half == 0) units.v[1][wc / kStatsUnit + u][row] = s;
+        }
+        if constexpr (KEEP) {
+            // through the wave's own part of the LDS, as in lmhead_dlogits_tile
+#pragma unroll
+            for (int j = 0; j < C::TN; ++j)
+#pragma unroll
+                for (int v = 0; v < 16; v += 4) {
+                    const f32x16& a = acc[i][j];
+                    *reinterpret_cast<u32x2*>(&sm.c16[row][wc + j * 32 + (v >> 2) * 8 + half * 4]) =
+                        pack_half4(a[v], a[v + 1], a[v + 2], a[v + 3]);
+                }
+            lds_wave_order();
+#pragma unroll
+            for (int q = 0; q < 32 / RPI; ++q) {
+                const int r = (wave / C::WN) * 32 + i * C::RS + q * RPI + lane / CPR;
+                const int c = wc + lane % CPR * 8;
+                const int64_t t = m0 + r, col = n0 + c;
+                if (t >= M || col >= V) continue;
+                // rows are padded to whole vectors
+                const u32x4 pk = *reinterpret_cast<const u32x4*>(&sm.c16[r][c]);
+                __builtin_nontemporal_store(pk, reinterpret_cast<u32x4*>(e + t * ld_e + col));
+            }
+        }
+    }
+    lds_ring_barrier();
+    for (int r = tid; r < C::BM && m0 + r < M; r += C::THREADS) {
+        float m = units.v[0][0][r], s = units.v[1][0][r], zs = units.v[2][0][r];
+#pragma unroll
+        for (int k = 1; k < kUnitsPerTile; ++k) {
+            m = fmaxf(m, units.v[0][k][r]);
+            s += units.v[1][k][r];
+            zs += units.v[2][k][r];
+        }
+        part[(m0 + r) * nvt + vt] = make_float4(m, s * 0x1p-15f, zs, 0.f);
+    }
+}
+
+// The block's rows are its first *n_rows - base: the tiles are laid over theirs, as in
+// lmhead_dlogits_kernel.
+template <class C, bool KEEP>
+__global__ void __launch_bounds__(C::THREADS)
+xent_tile_kernel(const uint16_t* __restrict__ h, int64_t M, int64_t ldh,
+                 const uint16_t* __restrict__ w, int64_t V, int64_t ldw, int64_t d,
+                 const int32_t* __restrict__ target, int64_t nvt, float4* __restrict__ part,
+                 float* __restrict__ z_y, uint16_t* __restrict__ e, int64_t ld_e,
+                 const int32_t* __restrict__ n_rows, int64_t base) {
+    __shared__ Units units;
+    const int64_t live = (int64_t)*n_rows - base;
+    M = live < M ? (live > 0 ? live : 0) : M;
+    with_row_tile<C>(M, nvt, [&](auto cfg, auto& sm, int64_t m0, int64_t vt) {
+        xent_tile<decltype(cfg), KEEP>(h, M, ldh, w, V, ldw, d, target, nvt, part, z_y, e, ld_e, sm,
+                                       units, m0, vt);
+    });
+}
+
+// The objective's constants.
+struct XentTerms {
+    float eps, lambda;
+};
+
+// A row's maximum, normaliser and sum.
+struct RowSums {
+    float m, s;
+    double z;
+};
+__device__ __forceinline__ RowSums joined(const RowSums& a, const RowSums& b) {
+    RowSums r = {fmaxf(a.m, b.m), 0.f, a.z + b.z};
+    // an empty part's s is 0, and its maximum may be that of both
+    r.s = (a.s == 0.f ? 0.f : a.s * expf(a.m - r.m)) + (b.s == 0.f ? 0.f : b.s * expf(b.m - r.m));
+    return r;
+}
+
+// One workgroup of THREADS per row r of the block (of its first *n_rows - base): merges the
+// row's triples (lane-strided in index order, then a butterfly, then the waves in order),
+// adds the target logit last as lmhead_merge_kernel does, and writes the row's loss to
+// tok_loss[map[r]]. With KEEP the row of e becomes dz / (1 - eps) in bf16, in place.
+template <int THREADS, bool KEEP>
+__global__ void __launch_bounds__(THREADS)
+xent_rows_kernel(const float4* __restrict__ part, const float* __restrict__ z_y, int64_t nvt,
+                 int64_t V, const int32_t* __restrict__ target, const int32_t* __restrict__ map,
+                 XentTerms terms, uint16_t* __restrict__ e, int64_t ld_e,
+                 float* __restrict__ tok_loss, const int32_t* __restrict__ n_rows, int64_t base) {
+    constexpr int WAVES = THREADS / 64;
+    __shared__ RowSums waves[WAVES];
+    const int tid = threadIdx.x, lane = tid & 63;
+    const int64_t r = blockIdx.x;
+    if (r >= (int64_t)*n_rows - base) return;
+    const int32_t y = target[r];
+    const int64_t chunks = (V + 7) / 8;
+    [[maybe_unused]] u32x4* row = KEEP ? reinterpret_cast<u32x4*>(e + r * ld_e) : nullptr;
+    RowSums x = {-INFINITY, 0.f, 0.0};
+    for (int64_t j = tid; j < nvt; j += THREADS) {
+        const float4 p = part[r * nvt + j];
+        x = joined(x, RowSums{p.x, p.y, (double)p.z});
+    }
+#pragma unroll
+    for (int off = 32; off >= 1; off >>= 1) {
+        const RowSums o = {__shfl_xor(x.m, off), __shfl_xor(x.s, off), __shfl_xor(x.z, off)};
+        // the lower lane's first, so that both lanes round the same
+        x = lane & off ? joined(o, x) : joined(x, o);
+    }
+    if constexpr (WAVES > 1) {
+        if (lane == 0) waves[tid >> 6] = x;
+        __syncthreads();
+        x = waves[0];
+        for (int k = 1; k < WAVES; ++k) x = joined(x, waves[k]);
+    }
+    // the target last: lse = M + log S, logp from -log1p(s_rest / e_y) when it dominates
+    const float zy = z_y[r];
+    // (x.s is 0 where there is no other column, a NaN where a logit is none)
+    const float M = x.s != 0.f ? fmaxf(x.m, zy) : zy;
+    const float sx = x.s != 0.f ? x.s * expf(x.m - M) : 0.f, ey = expf(zy - M);
+    const float ln_s = logf(sx + ey), lse = M + ln_s;
+    const float logp = sx < ey ? -log1pf(sx / ey) : (zy - M) - ln_s;
+    if (tid == 0) {
+        const double l = (double)lse;
+        double loss = -(double)logp * (1.0 - (double)terms.eps) + (double)terms.lambda * l * l;
+        if (terms.eps > 0.f) loss += (double)terms.eps * (l - x.z / (double)V);
+        tok_loss[map[r]] = (float)loss;
+    }
+    if constexpr (KEEP) {
+        const float keep = 1.f / (1.f - terms.eps), g = 1.f + 2.f * terms.lambda * lse;
+        const float flat = terms.eps / (float)V * keep, a = g * keep * 0x1p-15f;
+        // (p g - (1 - eps) - eps / V) / (1 - eps), p - 1 = expm1(log p)
+        const float dy =
+            (expm1f(logp) + terms.eps + 2.f * terms.lambda * lse * expf(logp)) * keep - flat;
+        typedef _Float16 h8 __attribute__((ext_vector_type(8)));
+        for (int64_t c = tid; c < chunks; c += THREADS) {
+            const h8 q = __builtin_bit_cast(h8, row[c]);
+            // the maximum of the chunk's tile, as the exponentials took it
+            const float m = part[r * nvt + c / (LmCfg::BN / 8)].x;
+            const float f = m == -INFINITY ? 0.f : a * expf(m - lse);
+            float v[8];
+#pragma unroll
+            for (int k = 0; k < 8; ++k) v[k] = fmaf((float)q[k], f, -flat);
+            if (c == y >> 3)
+#pragma unroll
+                for (int k = 0; k < 8; ++k) v[k] = k == (y & 7) ? dy : v[k];
+            row[c] = u32x4{pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]),
+                           pack_bf16x2(v[4], v[5]), pack_bf16x2(v[6], v[7])};
+        }
+    }
+}
+
+// One workgroup: the rows with a label in increasing order in map, their number n, and the gradients' factor (1 - eps) / n, or 1 - eps for a sum; 0 without labels.
+constexpr int kLabelThreads = 1024;
+__global__ void __launch_bounds__(kLabelThreads)
+xent_labels_kernel(const int32_t* __restrict__ target, int64_t T, int64_t V, float eps, int mean,
+                   int32_t* __restrict__ map, int32_t* __restrict__ count,
+                   int32_t* __restrict__ n_valid, float* __restrict__ scale) {
+    __shared__ int wave_n[2][kLabelThreads / 64];
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    int64_t base = 0;
+    for (int64_t t0 = 0, k = 0; t0 < T; t0 += kLabelThreads, ++k) {
+        const int64_t t = t0 + tid;
+        const bool keep = t < T && has_label(target[t], V);
+        const uint64_t ballot = __ballot(keep);
+        const int before = __popcll(ballot & ((uint64_t(1) << lane) - 1));
+        if (lane == 0) wave_n[k & 1][wave] = __popcll(ballot);
+        __syncthreads();  // the other half is free: its readers are past the last barrier
+        int off = 0, total = 0;
+        for (int w = 0; w < kLabelThreads / 64; ++w) {
+            off += w < wave ? wave_n[k & 1][w] : 0;
+            total += wave_n[k & 1][w];
+        }
+        if (keep) map[base + off + before] = (int32_t)t;
+        base += total;
+    }
+    if (tid) return;
+    count[0] = (int32_t)base;
+    n_valid[0] = (int32_t)base;
+    const double f = 1.0 - (double)eps;
+    scale[0] = base == 0 ? 0.f : (float)(mean ? f / (double)base : f);
+}
+
+// Row i < count: hidden row map[i] and its target; and row i of dh (unless null) and of
+// tok_loss set to 0 where it has no label. One workgroup per row, grid-stride.
+__global__ void __launch_bounds__(128)
+xent_gather_kernel(const int32_t* __restrict__ map, const int32_t* __restrict__ count, int64_t T,
+                   int64_t V, const uint16_t* __restrict__ h, int64_t ld_h, int64_t d,
+                   const int32_t* __restrict__ target, uint16_t* __restrict__ h_c,
+                   int32_t* __restrict__ target_c, float* __restrict__ tok_loss,
+                   uint16_t* __restrict__ dh, int64_t ld_dh) {
+    const int64_t n = count[0];
+    for (int64_t i = blockIdx.x; i < T; i += gridDim.x) {
+        if (!has_label(target[i], V)) {
+            if (dh)
+                for (int64_t c = threadIdx.x; c < d; c += 128) dh[i * ld_dh + c] = 0;
+            if (threadIdx.x == 0) tok_loss[i] = 0.f;
+        }
+        if (i >= n) continue;
+        const int64_t t = map[i];
+        const u32x4* src = reinterpret_cast<const u32x4*>(h + t * ld_h);
+        u32x4* dst = reinterpret_cast<u32x4*>(h_c + i * d);
+        for (int64_t j = threadIdx.x; j < d / 8; j += 128) dst[j] = src[j];
+        if (threadIdx.x == 0) target_c[i] = target[t];
+    }
+}
+
+// One workgroup: the loss, summed in fp64 in a fixed order.
+constexpr int kLossThreads = 1024;
+__global__ void __launch_bounds__(kLossThreads)
+xent_loss_kernel(const float* __restrict__ tok_loss, int64_t T, int mean,
+                 const int32_t* __restrict__ count, float* __restrict__ loss) {
+    __shared__ double waves[kLossThreads / 64];
+    const int tid = threadIdx.x;
+    double x = 0.0;
+    for (int64_t t = tid; t < T; t += kLossThreads) x += (double)tok_loss[t];
+#pragma unroll
+    for (int off = 32; off >= 1; off >>= 1) x += __shfl_xor(x, off);
+    if ((tid & 63) == 0) waves[tid >> 6] = x;
+    __syncthreads();
+    if (tid) return;
+    for (int k = 1; k < kLossThreads / 64; ++k) x += waves[k];
+    const int n = count[0];
+    loss[0] = (float)(mean && n > 0 ? x / (double)n : x);
+}
+
+__device__ __forceinline__ void scale_by(float& x, float f) { x *= f; }
+__device__ __forceinline__ void scale_by(uint16_t& x, float f) {
+    x = bf16_bits(__uint_as_float((uint32_t)x << 16) * f);
+}
+
+// x *= *factor, rows of it by a workgroup, grid-stride; 16 bytes a lane with VEC.
+constexpr int kScaleThreads = 256;
+template <class X, bool VEC>
+__global__ void __launch_bounds__(kScaleThreads)
+grad_scale_kernel(X* __restrict__ x, int64_t rows, int64_t cols, int64_t ld,
+                  const float* __restrict__ factor) {
+    const float f = *factor;
+    if (f == 1.f) return;
+    constexpr int N = VEC ? 16 / sizeof(X) : 1;
+    typedef X Some __attribute__((ext_vector_type(N)));
+    for (int64_t r = blockIdx.x; r < rows; r += gridDim.x)
+        for (int64_t c = (int64_t)threadIdx.x * N; c < cols; c += kScaleThreads * N) {
+            Some* p = reinterpret_cast<Some*>(x + r * ld + c);
+            Some v = *p;
+#pragma unroll
+            for (int k = 0; k < N; ++k) {
+                X one = v[k];
+                scale_by(one, f);
+                v[k] = one;
+            }
+            *p = v;
+        }
+}
+
+constexpr int64_t kRowBlocksMost = 65536;
+int64_t ceil8(int64_t x) { return (x + 7) / 8 * 8; }
+
+// Where a call's parts sit in the workspace (byte offsets, each 256-byte aligned).
+struct XentPlan {
+    int64_t rows;   // a block's
+    bool acc_w;     // dW summed over blocks in fp32
+    int64_t ksplit; // parts of dh's sum over the vocabulary
+    size_t e, part, z_y, count, scale, map, target_c, h_c, accw, parts, total;
+};
+
+// total = 0 when the sizes do not fit the address arithmetic. rows: a block's (grad), or
+// T (forward alone).
+XentPlan plan_xent(int64_t T, int64_t d, int64_t V, int64_t rows, bool grad, bool want_w) {
+    XentPlan P = {};
+    P.rows = rows < T ? rows : T;
+    P.acc_w = grad && want_w && P.rows < T;
+    P.ksplit = grad ? lmhead::dh_parts(P.rows, d, V) : 1;
+    const double big = double(int64_t(1) << 60), nvt = (double)vocab_tiles(V);
+    if ((double)P.rows * (double)ceil8(V) * 2 > big || (double)V * (double)d * 4 > big ||
+        (double)T * (double)d * 2 > big || (double)P.rows * nvt * 16 > big)
+        return P;
+    size_t end = 0;
+    auto take = [&](size_t bytes) {
+        const size_t at = (end + 255) / 256 * 256;
+        end = at + bytes;
+        return at;
+    };
+    P.count = take(4);
+    P.scale = take(4);
+    P.part = take((size_t)P.rows * (size_t)vocab_tiles(V) * sizeof(float4));
+    P.z_y = take((size_t)P.rows * 4);
+    P.map = take((size_t)T * 4);
+    P.target_c = take((size_t)T * 4);
+    P.h_c = take((size_t)T * (size_t)d * 2);
+    if (grad) P.e = take((size_t)P.rows * (size_t)ceil8(V) * 2);
+    if (P.acc_w) P.accw = take((size_t)V * (size_t)d * 4);
+    if (P.ksplit > 1) P.parts = take((size_t)P.ksplit * (size_t)P.rows * (size_t)d * 4);
+    P.total = end;
+    return P;
+}
+
+bool bad_terms(const dart_xent_config_t* c) {
+    return !c || !(c->label_smoothing >= 0.f) || !(c->label_smoothing < 1.f) ||
+           !(c->z_loss >= 0.f) || isinf(c->z_loss) ||
+           (c->reduction != DART_XENT_MEAN && c->reduction != DART_XENT_SUM);
+}
+
+bool bad_inputs(const void* hidden, int64_t T, int64_t d, int64_t ld_h, const void* weight,
+                int64_t V, int64_t ld_w, const int32_t* target) {
+    if (!hidden || !weight || !target) return true;
+    if (T < 1 || V < 1 || d < 8 || T > 0x7FFFFFFFll || V > 0x7FFFFFFFll || d > 0x7FFFFFFFll)
+        return true;
+    if (d % 8 || ld_h < d || ld_w < d || ld_h % 8 || ld_w % 8) return true;
+    return reinterpret_cast<uintptr_t>(hidden) % 16 || reinterpret_cast<uintptr_t>(weight) % 16;
+}
+
+// The whole call; without grads the loss alone.
+struct XentGrads {
+    void* dh;
+    int64_t ld_dh;
+    void* dw;
+    int64_t ld_dw;
+};
+dart_status_t run_xent(const uint16_t* h, int64_t T, int64_t d, int64_t ld_h, const uint16_t* w,
+                       int64_t V, int64_t ld_w, const int32_t* target,
+                       const dart_xent_config_t& config, float* loss, float* tok_loss,
+                       int32_t* n_valid, const XentGrads* grads, const XentPlan& P, char* ws,
+                       hipStream_t stream) {
+    const int64_t nvt = vocab_tiles(V);
+    const int mean = config.reduction == DART_XENT_MEAN;
+    const XentTerms terms = {config.label_smoothing, config.z_loss};
+    int32_t* count = reinterpret_cast<int32_t*>(ws + P.count);
+    float* scale = reinterpret_cast<float*>(ws + P.scale);
+    float4* part = reinterpret_cast<float4*>(ws + P.part);
+    float* z_y = reinterpret_cast<float*>(ws + P.z_y);
+    int32_t* map = reinterpret_cast<int32_t*>(ws + P.map);
+    uint16_t* h_c = reinterpret_cast<uint16_t*>(ws + P.h_c);
+    int32_t* target_c = reinterpret_cast<int32_t*>(ws + P.target_c);
+    hipLaunchKernelGGL(xent_labels_kernel, dim3(1), dim3(kLabelThreads), 0, stream, target, T, V,
+                       config.label_smoothing, mean, map, count, n_valid, scale);
+    hipLaunchKernelGGL(xent_gather_kernel, dim3((unsigned)(T < kRowBlocksMost ? T : kRowBlocksMost)),
+                       dim3(128), 0, stream, map, count, T, V, h, ld_h, d, target, h_c, target_c,
+                       tok_loss, grads ? static_cast<uint16_t*>(grads->dh) : nullptr,
+                       grads ? grads->ld_dh : 0);
+    uint16_t* e = grads ? reinterpret_cast<uint16_t*>(ws + P.e) : nullptr;
+    const int64_t ld_e = ceil8(V);
+    float* parts = P.ksplit > 1 ? reinterpret_cast<float*>(ws + P.parts) : nullptr;
+    const Grad dh{grads ? grads->dh : nullptr, grads ? grads->ld_dh : 0, true};
+    const Grad dw{grads ? grads->dw : nullptr, grads ? grads->ld_dw : 0, true};
+    const Grad sum_w = P.acc_w ? Grad{ws + P.accw, d, false} : dw;
+    for (int64_t r0 = 0; r0 < T; r0 += P.rows) {
+        const int64_t rows = T - r0 < P.rows ? T - r0 : P.rows;
+        const uint16_t* hr = h_c + r0 * d;
+        with_tile<>(tile_rows(rows, V, d <= 1024 ? 57 : 54), rows, V, [&](auto cfg) {
+            using C = decltype(cfg);
+            const dim3 grid((unsigned)((rows + C::BM - 1) / C::BM * nvt));
+            if (grads)
+                hipLaunchKernelGGL((xent_tile_kernel<C, true>), grid, dim3(C::THREADS), 0, stream,
+                                   hr, rows, d, w, V, ld_w, d, target_c + r0, nvt, part, z_y, e,
+                                   ld_e, count, r0);
+            else
+                hipLaunchKernelGGL((xent_tile_kernel<C, false>), grid, dim3(C::THREADS), 0, stream,
+                                   hr, rows, d, w, V, ld_w, d, target_c + r0, nvt, part, z_y, e,
+                                   ld_e, count, r0);
+        });
+        if (!grads) {
+            hipLaunchKernelGGL((xent_rows_kernel<64, false>), dim3((unsigned)rows), dim3(64), 0,
+                               stream, part, z_y, nvt, V, target_c + r0, map + r0, terms, e, ld_e,
+                               tok_loss, count, r0);
+            continue;
+        }
+        hipLaunchKernelGGL((xent_rows_kernel<512, true>), dim3((unsigned)rows), dim3(512), 0, stream,
+                           part, z_y, nvt, V, target_c + r0, map + r0, terms, e, ld_e, tok_loss,
+                           count, r0);
+        const dart_status_t st = lmhead::launch_bwd_gemms(
+            e, ld_e, rows, V, w, ld_w, hr, d, d, parts && dh.p ? Grad{parts, d, false} : dh, false,
+            parts ? P.ksplit : 1, P.rows * d, sum_w, P.acc_w && r0 > 0, stream, parts ? nullptr : map + r0,
+            count, r0, scale);
+        if (st != DART_OK) return st;
+        if (parts && dh.p)
+            lmhead::launch_sum_parts(parts, P.ksplit, P.rows * d, rows, d, map + r0, dh, count, r0,
+                                     stream);
+    }
+    if (P.acc_w) lmhead::launch_to_bf16(reinterpret_cast<float*>(ws + P.accw), V, d, dw, stream);
+    hipLaunchKernelGGL(xent_loss_kernel, dim3(1), dim3(kLossThreads), 0, stream, tok_loss, T, mean,
+                       count, loss);
+    return hipGetLastError() == hipSuccess ? DART_OK : DART_ERR_HIP;
+}
+
+// Launch limits: the tiles of 256 rows, one workgroup of 512 per row of a block, and the
+// tiles' 32-bit row offsets.
+bool too_large(int64_t rows, int64_t V, int64_t ld_h, int64_t ld_w) {
+    return !grid_fits((rows + LmCfg::BM - 1) / LmCfg::BM * vocab_tiles(V), LmCfg::THREADS) ||
+           !grid_fits(rows, 512) || ld_h > kMaxLd || ld_w > kMaxLd;
+}
+
+}  // namespace
+
+extern "C" {
+
+size_t dart_lmhead_xent_fwd_workspace_bytes(int64_t T, int64_t d, int64_t V) {
+    if (T < 1 || d < 1 || V < 1 || T > 0x7FFFFFFFll || d > 0x7FFFFFFFll || V > 0x7FFFFFFFll) return 0;
+    return plan_xent(T, d, V, T, false, false).total;
+}
+
+size_t dart_lmhead_xent_workspace_bytes(int64_t T, int64_t d, int64_t V, int64_t chunk_rows) {
+    if (T < 1 || d < 1 || V < 1 || chunk_rows < 1 || T > 0x7FFFFFFFll || d > 0x7FFFFFFFll ||
+        V > 0x7FFFFFFFll)
+        return 0;
+    return plan_xent(T, d, V, chunk_rows, true, true).total;
+}
+
+dart_status_t dart_lmhead_xent_fwd(const void* hidden, int64_t T, int64_t d, int64_t ld_h,
+                                   const void* weight, int64_t V, int64_t ld_w,
+                                   const int32_t* target, const dart_xent_config_t* config,
+                                   float* loss, float* tok_loss, int32_t* n_valid, void* workspace,
+                                   size_t workspace_bytes, hipStream_t stream) {
+    if (bad_inputs(hidden, T, d, ld_h, weight, V, ld_w, target) || bad_terms(config) || !loss ||
+        !tok_loss || !n_valid || !workspace || reinterpret_cast<uintptr_t>(workspace) % 16)
+        return DART_ERR_INVALID_ARG;
+    if (too_large(T, V, ld_h, ld_w)) return DART_ERR_UNSUPPORTED;
+    const XentPlan P = plan_xent(T, d, V, T, false, false);
+    if (P.total == 0) return DART_ERR_UNSUPPORTED;
+    if (workspace_bytes < P.total) return DART_ERR_INVALID_ARG;
+    if (const dart_status_t ck = dart_check::run(
+            stream, {{dart_check::Item::Labels, target, T, V}}); ck != DART_OK)
+        return ck;
+    return run_xent(static_cast<const uint16_t*>(hidden), T, d, ld_h,
+                    static_cast<const uint16_t*>(weight), V, ld_w, target, *config, loss, tok_loss,
+                    n_valid, nullptr, P, static_cast<char*>(workspace), stream);
+}
+
+dart_status_t dart_lmhead_xent_fwd_bwd(const void* hidden, int64_t T, int64_t d, int64_t ld_h,
+                                       const void* weight, int64_t V, int64_t ld_w,
+                                       const int32_t* target, const dart_xent_config_t* config,
+                                       float* loss, float* tok_loss, int32_t* n_valid,
+                                       void* dhidden, int64_t ld_dh, void* dweight, int64_t ld_dw,
+                                       int64_t chunk_rows, void* workspace, size_t workspace_bytes,
+                                       hipStream_t stream) {
+    if (bad_inputs(hidden, T, d, ld_h, weight, V, ld_w, target) || bad_terms(config) || !loss ||
+        !tok_loss || !n_valid || !workspace || reinterpret_cast<uintptr_t>(workspace) % 16)
+        return DART_ERR_INVALID_ARG;
+    if ((!dhidden && !dweight) || (dhidden && ld_dh < d) || (dweight && ld_dw < d) ||
+        chunk_rows < 1 || reinterpret_cast<uintptr_t>(dhidden) % 2 ||
+        reinterpret_cast<uintptr_t>(dweight) % 2)
+        return DART_ERR_INVALID_ARG;
+    const int64_t rows = chunk_rows < T ? chunk_rows : T;
+    if (too_large(rows, V, ld_h, ld_w) || ceil8(V) > kMaxLd || (dhidden && ld_dh > kMaxLd) ||
+        (dweight && ld_dw > kMaxLd))
+        return DART_ERR_UNSUPPORTED;
+    const XentPlan P = plan_xent(T, d, V, rows, true, dweight != nullptr);
+    if (P.total == 0) return DART_ERR_UNSUPPORTED;
+    if (workspace_bytes < P.total) return DART_ERR_INVALID_ARG;
+    if (const dart_status_t ck = dart_check::run(
+            stream, {{dart_check::Item::Labels, target, T, V}}); ck != DART_OK)
+        return ck;
+    const XentGrads grads = {dhidden, dhidden ? ld_dh : 0, dweight, dweight ? ld_dw : 0};
+    return run_xent(static_cast<const uint16_t*>(hidden), T, d, ld_h,
+                    static_cast<const uint16_t*>(weight), V, ld_w, target, *config, loss, tok_loss,
+                    n_valid, &grads, P, static_cast<char*>(workspace), stream);
+}
+
+dart_status_t dart_grad_scale(void* x, dart_dtype_t dtype, int64_t rows, int64_t cols, int64_t ld,
+                              const float* factor, hipStream_t stream) {
+    const size_t size = dtype == DART_BF16 ? 2 : 4;
+    if ((dtype != DART_BF16 && dtype != DART_F32) || !x || !factor || rows < 1 || cols < 1 ||
+        rows > 0x7FFFFFFFll || cols > 0x7FFFFFFFll || ld < cols ||
+        reinterpret_cast<uintptr_t>(x) % size || reinterpret_cast<uintptr_t>(factor) % 4)
+        return DART_ERR_INVALID_ARG;
+    const bool vec = reinterpret_cast<uintptr_t>(x) % 16 == 0 && ld * (int64_t)size % 16 == 0 &&
+                     cols * (int64_t)size % 16 == 0;
+    const dim3 grid((unsigned)(rows < kRowBlocksMost ? rows : kRowBlocksMost)), block(kScaleThreads);
+    auto launch = [&](auto kernel, auto* p) {
+        hipLaunchKernelGGL(kernel, grid, block, 0, stream, p, rows, cols, ld, factor);
+    };
+    if (dtype == DART_BF16)
+        vec ? launch(grad_scale_kernel<uint16_t, true>, static_cast<uint16_t*>(x))
+            : launch(grad_scale_kernel<uint16_t, false>, static_cast<uint16_t*>(x));
+    else
+        vec ? launch(grad_scale_kernel<float, true>, static_cast<float*>(x))
+            : launch(grad_scale_kernel<float, false>, static_cast<float*>(x));
+    return hipGetLastError() == hipSuccess ? DART_OK : DART_ERR_HIP;
+}
+
+}  // extern "C"
