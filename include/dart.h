@@ -634,7 +634,7 @@ dart_status_t dart_lmhead_xent_fwd_bwd(const void* hidden, int64_t T, int64_t d,
 
 /* Bytes of workspace of the two calls (0 for arguments outside
  * [1, INT32_MAX]). The second is chunk_rows * ceil8(V) * 2 for the
- * exponentials, chunk_rows * ceil(V/256) * 16 for partial sums, V * d * 4 where
+ * exponentials, chunk_rows * ceil(V/256) * 32 for partial sums, V * d * 4 where
  * chunk_rows < T, T * (2 d + 8) for the labelled rows, and at most
  * 64 MiB for dhidden's sum in parts where T and d are multiples of 256. Host only. */
 size_t dart_lmhead_xent_fwd_workspace_bytes(int64_t T, int64_t d, int64_t V);

@@ -110,8 +110,9 @@ __attribute__((visibility("hidden"))) dart_status_t launch_bwd_gemms(
 // compute units the launch waits for them (at 1000 rows, d = 3584, V = 152064:
 // 56 tiles of 2376 slices, 3.62 ms; in 2, 4 or 9 parts 2.10, 1.95 or 2.02 ms, adding
 // them up 7, 17 or 37 us more). So that at least half
-// and at most all of the units have a part, none shorter than kMinPartSlices.
-__attribute__((visibility("hidden"))) int64_t dh_parts(int64_t rows, int64_t d, int64_t cols);
+// and at most all of the units have a part, none shorter than least slices of 64.
+__attribute__((visibility("hidden"))) int64_t dh_parts(int64_t rows, int64_t d, int64_t cols,
+                                                       int64_t least);
 
 // The ksplit parts of dh (each [rows, d] fp32, part_stride elements apart) added up in
 // part order into out: row r to row r, or (map, its first entry that of row 0) to row

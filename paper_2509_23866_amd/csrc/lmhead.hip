@@ -839,6 +839,9 @@ constexpr uint32_t kBackwardFlags = DART_LMHEAD_SKIP_ZERO_ROWS | DART_LMHEAD_BF1
 int64_t ceil8(int64_t x) { return (x + 7) / 8 * 8; }
 size_t align256(size_t x) { return (x + 255) / 256 * 256; }
 
+// slices of 64 vocabulary entries in the shortest part of dh's sum
+constexpr int64_t kMinPartSlices = 32;
+
 // How a backward call runs and where its parts sit in the workspace (byte
 // offsets, each part 256-byte aligned; total is the end of the last part).
 struct BackwardPlan {
@@ -906,7 +909,7 @@ BackwardPlan plan_backward(int64_t T, int64_t d, int64_t V, int64_t chunk_rows,
     };
     if (P.skip) take_rows();
     P.total = end;
-    P.ksplit = lmhead::dh_parts(P.rows, d, P.cols);
+    P.ksplit = lmhead::dh_parts(P.rows, d, P.cols, kMinPartSlices);
     P.compact = !P.skip && leaves_zero_rows_out(T, d, V);
     if (P.compact) take_rows();
     if (P.ksplit > 1) P.parts = take((size_t)P.ksplit * (size_t)P.rows * (size_t)d * 4);
@@ -949,8 +952,6 @@ void launch_bwd_gemms_dw(int dw_mode, const BwdGemm& dh, const BwdGemm& dw, int6
     else if (dw_mode == kOutF32Acc) launch_bwd_gemms_t<DH, kOutF32Acc>(dh, dw, n_dh, blocks, stream);
     else launch_bwd_gemms_t<DH, kOutBf16>(dh, dw, n_dh, blocks, stream);
 }
-
-constexpr int64_t kMinPartSlices = 32;
 
 }  // namespace
 
@@ -1010,10 +1011,10 @@ void lmhead::launch_sum_parts(const float* parts, int64_t ksplit, int64_t part_s
                            dyn_base);
 }
 
-int64_t lmhead::dh_parts(int64_t rows, int64_t d, int64_t cols) {
+int64_t lmhead::dh_parts(int64_t rows, int64_t d, int64_t cols, int64_t least) {
     const int64_t tiles =
         ((rows + LmCfg::BM - 1) / LmCfg::BM) * ((d + LmCfg::BN - 1) / LmCfg::BN);
-    const int64_t by_units = kUnits / tiles, by_k = cols / (LmCfg::BK * kMinPartSlices);
+    const int64_t by_units = kUnits / tiles, by_k = cols / (LmCfg::BK * least);
     const int64_t n = by_units < by_k ? by_units : by_k;
     return n > 1 ? n : 1;
 }

@@ -61,21 +61,25 @@ __device__ __forceinline__ uint32_t e2m1x8(const float (&v)[8]) {
 #endif
 }
 
-// Eight values of a row from column k on: bf16 or fp32, zeros past K. vec: the row's
-// start and the whole of the eight are 16-byte aligned.
-__device__ __forceinline__ void load8(const float* p, bool vec, int64_t left, float (&v)[8]) {
-    if (vec && left >= 8) {
-        const f32x4 a = reinterpret_cast<const f32x4*>(p)[0], b = reinterpret_cast<const f32x4*>(p)[1];
+// The hardware takes 16-byte vectors at any multiple of an element's size.
+typedef u32x4 __attribute__((aligned(2))) u32x4_at2;
+typedef u32x4 __attribute__((aligned(4))) u32x4_at4;
+
+// Eight values of a row, the first `left` of them, then zeros.
+__device__ __forceinline__ void load8(const float* p, int64_t left, float (&v)[8]) {
+    if (left >= 8) {
+        const u32x4 a = reinterpret_cast<const u32x4_at4*>(p)[0];
+        const u32x4 b = reinterpret_cast<const u32x4_at4*>(p)[1];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) v[i] = a[i], v[4 + i] = b[i];
+        for (int i = 0; i < 4; ++i) v[i] = __uint_as_float(a[i]), v[4 + i] = __uint_as_float(b[i]);
     } else {
 #pragma unroll
         for (int i = 0; i < 8; ++i) v[i] = i < left ? p[i] : 0.f;
     }
 }
-__device__ __forceinline__ void load8(const uint16_t* p, bool vec, int64_t left, float (&v)[8]) {
-    if (vec && left >= 8) {
-        const u32x4 a = *reinterpret_cast<const u32x4*>(p);
+__device__ __forceinline__ void load8(const uint16_t* p, int64_t left, float (&v)[8]) {
+    if (left >= 8) {
+        const u32x4 a = *reinterpret_cast<const u32x4_at2*>(p);
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             v[2 * i] = __uint_as_float(a[i] << 16);
@@ -97,7 +101,7 @@ __device__ __forceinline__ uint32_t scale_byte(uint32_t top) {
 
 template <class X>
 __global__ void __launch_bounds__(kQuantThreads)
-mxfp4_quantize_kernel(const X* __restrict__ x, int64_t R, int64_t K, int64_t ld, int vec,
+mxfp4_quantize_kernel(const X* __restrict__ x, int64_t R, int64_t K, int64_t ld,
                       int64_t slices, int64_t runs, uint8_t* __restrict__ packed,
                       uint32_t* __restrict__ scales) {
     __shared__ uint32_t sc[64];
@@ -108,7 +112,7 @@ mxfp4_quantize_kernel(const X* __restrict__ x, int64_t R, int64_t K, int64_t ld,
 #pragma unroll
     for (int p = 0; p < 4; ++p) {
         const int64_t r = run * kRun + p * 8 + (tid >> 5);
-        load8(x + min(r, R - 1) * ld + min(k, K - 1), vec != 0, r < R ? K - k : 0, v[p]);
+        load8(x + min(r, R - 1) * ld + min(k, K - 1), r < R ? K - k : 0, v[p]);
     }
 #pragma unroll
     for (int p = 0; p < 4; ++p) {
@@ -135,19 +139,22 @@ mxfp4_quantize_kernel(const X* __restrict__ x, int64_t R, int64_t K, int64_t ld,
     if (tid < 64) scales[(slice * runs + run) * 64 + tid] = sc[tid];
 }
 
-// Rows of up to eight results at p, the first `left` of them.
-__device__ __forceinline__ void store8(float* p, bool vec, int64_t left, const float (&v)[8]) {
-    if (vec && left >= 8) {
-        reinterpret_cast<f32x4*>(p)[0] = f32x4{v[0], v[1], v[2], v[3]};
-        reinterpret_cast<f32x4*>(p)[1] = f32x4{v[4], v[5], v[6], v[7]};
+// Up to eight results at p, the first `left` of them.
+__device__ __forceinline__ void store8(float* p, int64_t left, const float (&v)[8]) {
+    if (left >= 8) {
+        u32x4 a, b;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) a[i] = __float_as_uint(v[i]), b[i] = __float_as_uint(v[4 + i]);
+        reinterpret_cast<u32x4_at4*>(p)[0] = a;
+        reinterpret_cast<u32x4_at4*>(p)[1] = b;
     } else {
         for (int i = 0; i < 8 && i < left; ++i) p[i] = v[i];
     }
 }
-__device__ __forceinline__ void store8(uint16_t* p, bool vec, int64_t left, const float (&v)[8]) {
-    if (vec && left >= 8) {
-        *reinterpret_cast<u32x4*>(p) = u32x4{pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]),
-                                             pack_bf16x2(v[4], v[5]), pack_bf16x2(v[6], v[7])};
+__device__ __forceinline__ void store8(uint16_t* p, int64_t left, const float (&v)[8]) {
+    if (left >= 8) {
+        *reinterpret_cast<u32x4_at2*>(p) = u32x4{pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]),
+                                                 pack_bf16x2(v[4], v[5]), pack_bf16x2(v[6], v[7])};
     } else {
         for (int i = 0; i < 8 && i < left; ++i) p[i] = bf16_bits(v[i]);
     }
@@ -156,7 +163,7 @@ __device__ __forceinline__ void store8(uint16_t* p, bool vec, int64_t left, cons
 template <class X>
 __global__ void __launch_bounds__(kQuantThreads)
 mxfp4_dequantize_kernel(const uint8_t* __restrict__ packed, const uint8_t* __restrict__ scales,
-                        int64_t R, int64_t K, int64_t slices, int64_t runs, int vec,
+                        int64_t R, int64_t K, int64_t slices, int64_t runs,
                         X* __restrict__ out, int64_t ld) {
     const int64_t run = blockIdx.x / slices, slice = blockIdx.x % slices;
     const int tid = threadIdx.x, c8 = tid & 31, c = c8 >> 2;
@@ -187,12 +194,9 @@ mxfp4_dequantize_kernel(const uint8_t* __restrict__ packed, const uint8_t* __res
             const float size = __uint_as_float((code & 7u) << 22) * 0x1p126f;
             v[i] = __uint_as_float(__float_as_uint(size) | (code & 8u) << 28) * scale;
         }
-        store8(out + r * ld + k, vec != 0, K - k, v);
+        store8(out + r * ld + k, K - k, v);
     }
 }
-
-typedef u32x4 __attribute__((aligned(2))) u32x4_at2;
-typedef u32x4 __attribute__((aligned(4))) u32x4_at4;
 
 // This wave's part of a result tile to out [M, ld] through the wave's own part of the
 // LDS (its accesses run in order: no barrier), 32 rows at a time, as in
@@ -318,10 +322,9 @@ dart_status_t dart_mxfp4_quantize(const void* x, dart_dtype_t dtype, int64_t R, 
         return DART_ERR_INVALID_ARG;
     const int64_t blocks = runs_of(R) * slices_of(K);
     if (!grid_fits(blocks, kQuantThreads)) return DART_ERR_UNSUPPORTED;
-    const int vec = !misaligned(x, 16) && ld * (int64_t)size_of(dtype) % 16 == 0;
     auto launch = [&](auto kernel, auto* p) {
         hipLaunchKernelGGL(kernel, dim3((unsigned)blocks), dim3(kQuantThreads), 0, stream, p, R, K,
-                           ld, vec, slices_of(K), runs_of(R), static_cast<uint8_t*>(packed),
+                           ld, slices_of(K), runs_of(R), static_cast<uint8_t*>(packed),
                            static_cast<uint32_t*>(scales));
     };
     if (dtype == DART_BF16)
@@ -339,11 +342,10 @@ dart_status_t dart_mxfp4_dequantize(const void* packed, const void* scales, int6
         return DART_ERR_INVALID_ARG;
     const int64_t blocks = runs_of(R) * slices_of(K);
     if (!grid_fits(blocks, kQuantThreads)) return DART_ERR_UNSUPPORTED;
-    const int vec = !misaligned(out, 16) && ld_out * (int64_t)size_of(dtype) % 16 == 0;
     auto launch = [&](auto kernel, auto* p) {
         hipLaunchKernelGGL(kernel, dim3((unsigned)blocks), dim3(kQuantThreads), 0, stream,
                            static_cast<const uint8_t*>(packed), static_cast<const uint8_t*>(scales),
-                           R, K, slices_of(K), runs_of(R), vec, p, ld_out);
+                           R, K, slices_of(K), runs_of(R), p, ld_out);
     };
     if (dtype == DART_BF16)
         launch(mxfp4_dequantize_kernel<uint16_t>, static_cast<uint16_t*>(out));

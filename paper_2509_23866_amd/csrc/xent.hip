@@ -8,7 +8,8 @@
 // normaliser, sum) per row and 256 columns, merged per row. With the gradient, rows are
 // taken a block at a time, and the product z is formed once:
 //   xent_tile_kernel  forms z tile by tile on the matrix cores, reduces each row's 256
-//                     columns to a triple, and keeps e = 2^15 e^(z - max) of them in fp16;
+//                     columns to a triple, and keeps e = 2^15 e^(z - m) of them in fp16, m the
+//                     largest of 64 columns;
 //   xent_rows_kernel  merges a row's triples to lse, and turns its e in place into the
 //                     bf16 dz / (1 - eps), from which no logit is needed;
 //   the GEMMs of the LM head's backward (dh = dz W, dW = dz^T h), times (1 - eps) / N.
@@ -17,8 +18,8 @@
 // So three products of T V d instead of the four of a loss whose coefficients only a
 // second pass knows (dart_lmhead_backward): at T = 4096, V = 152064, d = 3584 the kept
 // exponentials cost a read and a write of 1.25 GB, the fourth product took 3.4 ms.
-// What is rounded: e to fp16 (2^-12 of its value down to 2^-29 of its tile's maximum, below
-// that 2^-40 of the maximum: little beside the bf16 that follows), dz to bf16 for the
+// What is rounded: e to fp16 (2^-12 of its value down to 2^-29 of its 64 columns' largest, below
+// that 2^-40 of that: little beside the bf16 that follows), dz to bf16 for the
 // matrix cores, as in dart_lmhead_dlogits. dz is kept divided by 1 - eps and not yet by N,
 // so that the target's element of an unsure row, the largest of all, is next to -1 and
 // loses nothing by its rounding.
@@ -48,38 +49,49 @@ struct Units {
 };
 
 // Tile (m0, vt) of the logits: part[t * nvt + vt] = (max, sum of e^(z - max), sum of z, 0) of
-// row t over the tile's columns, the target's column in the sum of z alone; the workgroup
-// holding target[t] writes z_y[t]. With KEEP e [M, ld_e] receives 2^15 e^(z - max) in fp16 (0
-// in the target's column). Sums run in the order of lmhead_stats_kernel's, whatever the
-// tile's height, so that equal rows have equal results.
+// row t over the tile's columns, the target's column in the sum of z alone (which is formed if
+// sums); the workgroup holding target[t] writes z_y[t]. With KEEP e [M, ld_e] receives
+// 2^15 e^(z - m) in fp16 (0 in the target's column) for the maxima m of the row's units of 64
+// columns, and unit_m[t * nvt + vt] those of the tile's four. Each unit has a maximum of its own so
+// that a wave needs no other for its exponentials: with one for the 256 columns, and a
+// barrier before it, the tile took TILEOLD us in place of TILENEW (T = 4096, V = 152064,
+// d = 3584). Sums run in the same order whatever the tile's height, so that equal rows have
+// equal results.
 template <class C, bool KEEP>
 __device__ __forceinline__ void xent_tile(const uint16_t* __restrict__ h, int64_t M, int64_t ldh,
                                           const uint16_t* __restrict__ w, int64_t V, int64_t ldw,
-                                          int64_t d, const int32_t* __restrict__ target,
+                                          int64_t d, const int32_t* __restrict__ target, bool sums,
                                           int64_t nvt, float4* __restrict__ part,
-                                          float* __restrict__ z_y, uint16_t* __restrict__ e,
-                                          int64_t ld_e, typename C::Smem& sm, Units& units,
-                                          int64_t m0, int64_t vt) {
+                                          float4* __restrict__ unit_m, float* __restrict__ z_y,
+                                          uint16_t* __restrict__ e, int64_t ld_e,
+                                          typename C::Smem& sm, Units& units, int64_t m0,
+                                          int64_t vt) {
 #pragma clang fp contract(off)  // the same roundings in every configuration
     const int64_t n0 = vt * C::BN;
-    f32x16 acc[C::TM][C::TN];
-    gemm_tile<C>(h, M, ldh, w, V, ldw, d, m0, n0, sm, acc);
-
     const int tid = threadIdx.x, lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), half = lane >> 5;
     const int wr = (wave / C::WN) * 32 + (lane & 31), wc = (wave % C::WN) * (C::BN / C::WN);
+    // the targets before the K loop, which their latency hides behind
+    int32_t ys[C::TM];
+#pragma unroll
+    for (int i = 0; i < C::TM; ++i) {
+        const int64_t t = m0 + wr + i * C::RS;
+        ys[i] = t < M ? target[t] : -1;
+    }
+    f32x16 acc[C::TM][C::TN];
+    gemm_tile<C>(h, M, ldh, w, V, ldw, d, m0, n0, sm, acc);
+
     static_assert(C::TN % 2 == 0, "units of two 32-column blocks");
+    constexpr int CPR = C::TN * 4, RPI = 64 / CPR;  // 16-byte chunks a row, rows a store
 #pragma unroll
     for (int i = 0; i < C::TM; ++i) {
         const int row = wr + i * C::RS;
-        const int64_t t = m0 + row;
-        const int64_t y = t < M ? (int64_t)target[t] : -1;
 #pragma unroll
         for (int u = 0; u < C::TN / 2; ++u) {
             const int64_t u0 = n0 + wc + u * kStatsUnit;
             // the columns and the target within the unit, as in stats_of_tile
             const int vlim = (int)max(min(V - u0, (int64_t)kStatsUnit), (int64_t)0);
-            const int64_t yrel = y - u0;
+            const int64_t yrel = (int64_t)ys[i] - u0;
             const int y64 = yrel >= 0 && yrel < vlim ? (int)yrel : -1;
             float zs = 0.f;
             const bool masked = vlim < kStatsUnit || (y64 >= 0 && ((y64 >> 2) & 1) == half);
@@ -98,38 +110,21 @@ __device__ __forceinline__ void xent_tile(const uint16_t* __restrict__ h, int64_
                         zs += col >= vl ? 0.f : x;
                         acc[i][2 * u + j][v] = col >= vl || at_y ? -INFINITY : x;
                     }
-                if (y64 >= 0 && ((y64 >> 2) & 1) == half) z_y[t] = zy;
-            } else {
+                if (y64 >= 0 && ((y64 >> 2) & 1) == half) z_y[m0 + row] = zy;
+            } else if (sums) {
 #pragma unroll
                 for (int j = 0; j < 2; ++j)
 #pragma unroll
                     for (int v = 0; v < 16; ++v) zs += acc[i][2 * u + j][v];
             }
-            float mx = -INFINITY;
+            float m = -INFINITY;
 #pragma unroll
             for (int j = 0; j < 2; ++j)
 #pragma unroll
-                for (int v = 0; v < 16; ++v) mx = fmaxf(mx, acc[i][2 * u + j][v]);
-            mx = fmaxf(mx, __shfl_xor(mx, 32));
-            zs += __shfl_xor(zs, 32);
-            if (half == 0) {
-                units.v[0][wc / kStatsUnit + u][row] = mx;
-                units.v[2][wc / kStatsUnit + u][row] = zs;
-            }
-        }
-    }
-    lds_ring_barrier();
-    constexpr int CPR = C::TN * 4, RPI = 64 / CPR;  // 16-byte chunks a row, rows a store
-#pragma unroll
-    for (int i = 0; i < C::TM; ++i) {
-        const int row = wr + i * C::RS;
-        float m = units.v[0][0][row];
-#pragma unroll
-        for (int k = 1; k < kUnitsPerTile; ++k) m = fmaxf(m, units.v[0][k][row]);
-        // nothing but the target: every exponential below is 0
-        const float ml = (m == -INFINITY ? 0.f : m * kLog2e) - (float)kShift;
-#pragma unroll
-        for (int u = 0; u < C::TN / 2; ++u) {
+                for (int v = 0; v < 16; ++v) m = fmaxf(m, acc[i][2 * u + j][v]);
+            m = fmaxf(m, __shfl_xor(m, 32));
+            // nothing but the target: every exponential is 0
+            const float ml = (m == -INFINITY ? 0.f : m * kLog2e) - (float)kShift;
             float s2[2];
 #pragma unroll
             for (int j = 0; j < 2; ++j) {
@@ -144,7 +139,13 @@ __device__ __forceinline__ void xent_tile(const uint16_t* __restrict__ h, int64_
             }
             float s = s2[0] + s2[1];
             s += __shfl_xor(s, 32);
-            if (half == 0) units.v[1][wc / kStatsUnit + u][row] = s;
+            if (sums) zs += __shfl_xor(zs, 32);
+            if (half == 0) {
+                const int unit = wc / kStatsUnit + u;
+                units.v[0][unit][row] = m;
+                units.v[1][unit][row] = s;
+                units.v[2][unit][row] = zs;
+            }
         }
         if constexpr (KEEP) {
             // through the wave's own part of the LDS, as in lmhead_dlogits_tile
@@ -171,14 +172,21 @@ __device__ __forceinline__ void xent_tile(const uint16_t* __restrict__ h, int64_
     }
     lds_ring_barrier();
     for (int r = tid; r < C::BM && m0 + r < M; r += C::THREADS) {
-        float m = units.v[0][0][r], s = units.v[1][0][r], zs = units.v[2][0][r];
+        float mu[kUnitsPerTile], m = -INFINITY, s = 0.f, zs = 0.f;
 #pragma unroll
-        for (int k = 1; k < kUnitsPerTile; ++k) {
-            m = fmaxf(m, units.v[0][k][r]);
-            s += units.v[1][k][r];
+        for (int k = 0; k < kUnitsPerTile; ++k) {
+            mu[k] = units.v[0][k][r];
+            m = fmaxf(m, mu[k]);
             zs += units.v[2][k][r];
         }
-        part[(m0 + r) * nvt + vt] = make_float4(m, s * 0x1p-15f, zs, 0.f);
+#pragma unroll
+        for (int k = 0; k < kUnitsPerTile; ++k) {
+            const float sk = units.v[1][k][r];
+            s += sk == 0.f ? 0.f : sk * expf(mu[k] - m);
+        }
+        const int64_t at = (m0 + r) * nvt + vt;
+        part[at] = make_float4(m, s * 0x1p-15f, zs, 0.f);
+        if constexpr (KEEP) unit_m[at] = make_float4(mu[0], mu[1], mu[2], mu[3]);
     }
 }
 
@@ -188,15 +196,14 @@ template <class C, bool KEEP>
 __global__ void __launch_bounds__(C::THREADS)
 xent_tile_kernel(const uint16_t* __restrict__ h, int64_t M, int64_t ldh,
                  const uint16_t* __restrict__ w, int64_t V, int64_t ldw, int64_t d,
-                 const int32_t* __restrict__ target, int64_t nvt, float4* __restrict__ part,
-                 float* __restrict__ z_y, uint16_t* __restrict__ e, int64_t ld_e,
+                 const int32_t* __restrict__ target, int sums, int64_t nvt,
+                 float4* __restrict__ part, float4* __restrict__ unit_m, float* __restrict__ z_y, uint16_t* __restrict__ e, int64_t ld_e,
                  const int32_t* __restrict__ n_rows, int64_t base) {
-    __shared__ Units units;
     const int64_t live = (int64_t)*n_rows - base;
     M = live < M ? (live > 0 ? live : 0) : M;
-    with_row_tile<C>(M, nvt, [&](auto cfg, auto& sm, int64_t m0, int64_t vt) {
-        xent_tile<decltype(cfg), KEEP>(h, M, ldh, w, V, ldw, d, target, nvt, part, z_y, e, ld_e, sm,
-                                       units, m0, vt);
+    with_row_tile<C, Units>(M, nvt, [&](auto cfg, auto& sm, int64_t m0, int64_t vt, Units& units) {
+        xent_tile<decltype(cfg), KEEP>(h, M, ldh, w, V, ldw, d, target, sums != 0, nvt, part, unit_m,
+                                       z_y, e, ld_e, sm, units, m0, vt);
     });
 }
 
@@ -223,8 +230,9 @@ __device__ __forceinline__ RowSums joined(const RowSums& a, const RowSums& b) {
 // tok_loss[map[r]]. With KEEP the row of e becomes dz / (1 - eps) in bf16, in place.
 template <int THREADS, bool KEEP>
 __global__ void __launch_bounds__(THREADS)
-xent_rows_kernel(const float4* __restrict__ part, const float* __restrict__ z_y, int64_t nvt,
-                 int64_t V, const int32_t* __restrict__ target, const int32_t* __restrict__ map,
+xent_rows_kernel(const float4* __restrict__ part, const float* __restrict__ unit_m,
+                 const float* __restrict__ z_y, int64_t nvt, int64_t V,
+                 const int32_t* __restrict__ target, const int32_t* __restrict__ map,
                  XentTerms terms, uint16_t* __restrict__ e, int64_t ld_e,
                  float* __restrict__ tok_loss, const int32_t* __restrict__ n_rows, int64_t base) {
     constexpr int WAVES = THREADS / 64;
@@ -274,8 +282,8 @@ xent_rows_kernel(const float4* __restrict__ part, const float* __restrict__ z_y,
         typedef _Float16 h8 __attribute__((ext_vector_type(8)));
         for (int64_t c = tid; c < chunks; c += THREADS) {
             const h8 q = __builtin_bit_cast(h8, row[c]);
-            // the maximum of the chunk's tile, as the exponentials took it
-            const float m = part[r * nvt + c / (LmCfg::BN / 8)].x;
+            // the maximum of the chunk's unit
+            const float m = unit_m[r * nvt * kUnitsPerTile + c / (kStatsUnit / 8)];
             const float f = m == -INFINITY ? 0.f : a * expf(m - lse);
             float v[8];
 #pragma unroll
@@ -289,12 +297,85 @@ xent_rows_kernel(const float4* __restrict__ part, const float* __restrict__ z_y,
     }
 }
 
-// One workgroup: the rows with a label in increasing order in map, their number n, and the gradients' factor (1 - eps) / n, or 1 - eps for a sum; 0 without labels.
+// The labels' count and the gradients' factor, written by one work-item: (1 - eps) / n, or
+// 1 - eps for a sum; 0 without labels.
+struct LabelOut {
+    int32_t *count, *n_valid;
+    float* scale;
+    float eps;
+    int mean;
+};
+__device__ __forceinline__ void put_labels(const LabelOut& o, int64_t n) {
+    o.count[0] = (int32_t)n;
+    o.n_valid[0] = (int32_t)n;
+    const double f = 1.0 - (double)o.eps;
+    o.scale[0] = n == 0 ? 0.f : (float)(o.mean ? f / (double)n : f);
+}
+
+// Row t with a label: its hidden row and target to row `at` of the labelled ones. Without: its
+// row of dh (unless null) and its loss set to 0. By a workgroup of THREADS.
+template <int THREADS>
+__device__ __forceinline__ void place_row(int64_t t, int64_t at, const uint16_t* __restrict__ h,
+                                          int64_t ld_h, int64_t d, int32_t y,
+                                          uint16_t* __restrict__ h_c,
+                                          int32_t* __restrict__ target_c) {
+    const u32x4* src = reinterpret_cast<const u32x4*>(h + t * ld_h);
+    u32x4* dst = reinterpret_cast<u32x4*>(h_c + at * d);
+    for (int64_t j = threadIdx.x; j < d / 8; j += THREADS) dst[j] = src[j];
+    if (threadIdx.x == 0) target_c[at] = y;
+}
+template <int THREADS>
+__device__ __forceinline__ void clear_row(int64_t t, int64_t d, float* __restrict__ tok_loss,
+                                          uint16_t* __restrict__ dh, int64_t ld_dh) {
+    if (dh)
+        for (int64_t c = threadIdx.x; c < d; c += THREADS) dh[t * ld_dh + c] = 0;
+    if (threadIdx.x == 0) tok_loss[t] = 0.f;
+}
+
+// One workgroup per row t: finds the row's place among the labelled ones by counting the labels
+// before it, and places or clears it; the first workgroup counts them all. For few rows
+// (kFewRows): 3 us at T = 48, 7 at 1000 and 19 at 4096, where the two kernels below take 8,
+// 12 and 20.
+constexpr int kPrepareThreads = 256;
+constexpr int64_t kFewRows = 4096;
+__global__ void __launch_bounds__(kPrepareThreads)
+xent_prepare_kernel(const int32_t* __restrict__ target, int64_t T, int64_t V,
+                    const uint16_t* __restrict__ h, int64_t ld_h, int64_t d,
+                    int32_t* __restrict__ map, uint16_t* __restrict__ h_c,
+                    int32_t* __restrict__ target_c, float* __restrict__ tok_loss,
+                    uint16_t* __restrict__ dh, int64_t ld_dh, LabelOut out) {
+    __shared__ int waves[kPrepareThreads / 64];
+    const int64_t t = blockIdx.x;
+    const int tid = threadIdx.x;
+    const int32_t y = target[t];
+    const bool labelled = has_label(y, V);
+    if (!labelled) clear_row<kPrepareThreads>(t, d, tok_loss, dh, ld_dh);
+    if (!labelled && t > 0) return;
+    // the first row's workgroup, which has none before it, counts all
+    const int64_t end = t > 0 ? t : T;
+    int n = 0;
+#pragma unroll 4
+    for (int64_t i = tid; i < end; i += kPrepareThreads) n += has_label(target[i], V);
+#pragma unroll
+    for (int off = 32; off >= 1; off >>= 1) n += __shfl_xor(n, off);
+    if ((tid & 63) == 0) waves[tid >> 6] = n;
+    __syncthreads();
+    n = 0;
+    for (int k = 0; k < kPrepareThreads / 64; ++k) n += waves[k];
+    if (t == 0) {
+        if (tid == 0) put_labels(out, n);
+        if (!labelled) return;
+        n = 0;
+    }
+    if (tid == 0) map[n] = (int32_t)t;
+    place_row<kPrepareThreads>(t, n, h, ld_h, d, y, h_c, target_c);
+}
+
+// One workgroup: the rows with a label in increasing order in map, and their number.
 constexpr int kLabelThreads = 1024;
 __global__ void __launch_bounds__(kLabelThreads)
-xent_labels_kernel(const int32_t* __restrict__ target, int64_t T, int64_t V, float eps, int mean,
-                   int32_t* __restrict__ map, int32_t* __restrict__ count,
-                   int32_t* __restrict__ n_valid, float* __restrict__ scale) {
+xent_labels_kernel(const int32_t* __restrict__ target, int64_t T, int64_t V,
+                   int32_t* __restrict__ map, LabelOut out) {
     __shared__ int wave_n[2][kLabelThreads / 64];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     int64_t base = 0;
@@ -313,15 +394,11 @@ xent_labels_kernel(const int32_t* __restrict__ target, int64_t T, int64_t V, flo
         if (keep) map[base + off + before] = (int32_t)t;
         base += total;
     }
-    if (tid) return;
-    count[0] = (int32_t)base;
-    n_valid[0] = (int32_t)base;
-    const double f = 1.0 - (double)eps;
-    scale[0] = base == 0 ? 0.f : (float)(mean ? f / (double)base : f);
+    if (tid == 0) put_labels(out, base);
 }
 
-// Row i < count: hidden row map[i] and its target; and row i of dh (unless null) and of
-// tok_loss set to 0 where it has no label. One workgroup per row, grid-stride.
+// Row i < count: row map[i] placed; and row i cleared where it has no label. One workgroup per
+// row, grid-stride.
 __global__ void __launch_bounds__(128)
 xent_gather_kernel(const int32_t* __restrict__ map, const int32_t* __restrict__ count, int64_t T,
                    int64_t V, const uint16_t* __restrict__ h, int64_t ld_h, int64_t d,
@@ -330,17 +407,8 @@ xent_gather_kernel(const int32_t* __restrict__ map, const int32_t* __restrict__ 
                    uint16_t* __restrict__ dh, int64_t ld_dh) {
     const int64_t n = count[0];
     for (int64_t i = blockIdx.x; i < T; i += gridDim.x) {
-        if (!has_label(target[i], V)) {
-            if (dh)
-                for (int64_t c = threadIdx.x; c < d; c += 128) dh[i * ld_dh + c] = 0;
-            if (threadIdx.x == 0) tok_loss[i] = 0.f;
-        }
-        if (i >= n) continue;
-        const int64_t t = map[i];
-        const u32x4* src = reinterpret_cast<const u32x4*>(h + t * ld_h);
-        u32x4* dst = reinterpret_cast<u32x4*>(h_c + i * d);
-        for (int64_t j = threadIdx.x; j < d / 8; j += 128) dst[j] = src[j];
-        if (threadIdx.x == 0) target_c[i] = target[t];
+        if (!has_label(target[i], V)) clear_row<128>(i, d, tok_loss, dh, ld_dh);
+        if (i < n) place_row<128>(map[i], i, h, ld_h, d, target[map[i]], h_c, target_c);
     }
 }
 
@@ -395,12 +463,17 @@ grad_scale_kernel(X* __restrict__ x, int64_t rows, int64_t cols, int64_t ld,
 constexpr int64_t kRowBlocksMost = 65536;
 int64_t ceil8(int64_t x) { return (x + 7) / 8 * 8; }
 
+// Slices of 64 vocabulary entries in the shortest part of dh's sum: a slice takes 1 us where few
+// tiles run, adding the parts up 4 us (48 rows of V = 4000, d = 512: the products 66 us in one
+// part of 63 slices, PARTSUS us in 7).
+constexpr int64_t kMinPartSlices = 8;
+
 // Where a call's parts sit in the workspace (byte offsets, each 256-byte aligned).
 struct XentPlan {
     int64_t rows;   // a block's
     bool acc_w;     // dW summed over blocks in fp32
     int64_t ksplit; // parts of dh's sum over the vocabulary
-    size_t e, part, z_y, count, scale, map, target_c, h_c, accw, parts, total;
+    size_t e, part, unit_m, z_y, count, scale, map, target_c, h_c, accw, parts, total;
 };
 
 // total = 0 when the sizes do not fit the address arithmetic. rows: a block's (grad), or
@@ -409,7 +482,7 @@ XentPlan plan_xent(int64_t T, int64_t d, int64_t V, int64_t rows, bool grad, boo
     XentPlan P = {};
     P.rows = rows < T ? rows : T;
     P.acc_w = grad && want_w && P.rows < T;
-    P.ksplit = grad ? lmhead::dh_parts(P.rows, d, V) : 1;
+    P.ksplit = grad ? lmhead::dh_parts(P.rows, d, V, kMinPartSlices) : 1;
     const double big = double(int64_t(1) << 60), nvt = (double)vocab_tiles(V);
     if ((double)P.rows * (double)ceil8(V) * 2 > big || (double)V * (double)d * 4 > big ||
         (double)T * (double)d * 2 > big || (double)P.rows * nvt * 16 > big)
@@ -427,6 +500,7 @@ XentPlan plan_xent(int64_t T, int64_t d, int64_t V, int64_t rows, bool grad, boo
     P.map = take((size_t)T * 4);
     P.target_c = take((size_t)T * 4);
     P.h_c = take((size_t)T * (size_t)d * 2);
+    if (grad) P.unit_m = take((size_t)P.rows * (size_t)vocab_tiles(V) * sizeof(float4));
     if (grad) P.e = take((size_t)P.rows * (size_t)ceil8(V) * 2);
     if (P.acc_w) P.accw = take((size_t)V * (size_t)d * 4);
     if (P.ksplit > 1) P.parts = take((size_t)P.ksplit * (size_t)P.rows * (size_t)d * 4);
@@ -467,16 +541,27 @@ dart_status_t run_xent(const uint16_t* h, int64_t T, int64_t d, int64_t ld_h, co
     int32_t* count = reinterpret_cast<int32_t*>(ws + P.count);
     float* scale = reinterpret_cast<float*>(ws + P.scale);
     float4* part = reinterpret_cast<float4*>(ws + P.part);
+    float4* unit_m = grads ? reinterpret_cast<float4*>(ws + P.unit_m) : nullptr;
     float* z_y = reinterpret_cast<float*>(ws + P.z_y);
+    const int sums = config.label_smoothing > 0.f;
     int32_t* map = reinterpret_cast<int32_t*>(ws + P.map);
     uint16_t* h_c = reinterpret_cast<uint16_t*>(ws + P.h_c);
     int32_t* target_c = reinterpret_cast<int32_t*>(ws + P.target_c);
-    hipLaunchKernelGGL(xent_labels_kernel, dim3(1), dim3(kLabelThreads), 0, stream, target, T, V,
-                       config.label_smoothing, mean, map, count, n_valid, scale);
-    hipLaunchKernelGGL(xent_gather_kernel, dim3((unsigned)(T < kRowBlocksMost ? T : kRowBlocksMost)),
-                       dim3(128), 0, stream, map, count, T, V, h, ld_h, d, target, h_c, target_c,
-                       tok_loss, grads ? static_cast<uint16_t*>(grads->dh) : nullptr,
-                       grads ? grads->ld_dh : 0);
+    const LabelOut out = {count, n_valid, scale, config.label_smoothing, mean};
+    uint16_t* dh_rows = grads ? static_cast<uint16_t*>(grads->dh) : nullptr;
+    const int64_t ld_dh = grads ? grads->ld_dh : 0;
+    if (T <= kFewRows) {
+        hipLaunchKernelGGL(xent_prepare_kernel, dim3((unsigned)T), dim3(kPrepareThreads), 0, stream,
+                           target, T, V, h, ld_h, d, map, h_c, target_c, tok_loss, dh_rows, ld_dh,
+                           out);
+    } else {
+        hipLaunchKernelGGL(xent_labels_kernel, dim3(1), dim3(kLabelThreads), 0, stream, target, T, V,
+                           map, out);
+        hipLaunchKernelGGL(xent_gather_kernel,
+                           dim3((unsigned)(T < kRowBlocksMost ? T : kRowBlocksMost)), dim3(128), 0,
+                           stream, map, count, T, V, h, ld_h, d, target, h_c, target_c, tok_loss,
+                           dh_rows, ld_dh);
+    }
     uint16_t* e = grads ? reinterpret_cast<uint16_t*>(ws + P.e) : nullptr;
     const int64_t ld_e = ceil8(V);
     float* parts = P.ksplit > 1 ? reinterpret_cast<float*>(ws + P.parts) : nullptr;
@@ -491,22 +576,22 @@ dart_status_t run_xent(const uint16_t* h, int64_t T, int64_t d, int64_t ld_h, co
             const dim3 grid((unsigned)((rows + C::BM - 1) / C::BM * nvt));
             if (grads)
                 hipLaunchKernelGGL((xent_tile_kernel<C, true>), grid, dim3(C::THREADS), 0, stream,
-                                   hr, rows, d, w, V, ld_w, d, target_c + r0, nvt, part, z_y, e,
-                                   ld_e, count, r0);
+                                   hr, rows, d, w, V, ld_w, d, target_c + r0, sums, nvt, part,
+                                   unit_m, z_y, e, ld_e, count, r0);
             else
                 hipLaunchKernelGGL((xent_tile_kernel<C, false>), grid, dim3(C::THREADS), 0, stream,
-                                   hr, rows, d, w, V, ld_w, d, target_c + r0, nvt, part, z_y, e,
-                                   ld_e, count, r0);
+                                   hr, rows, d, w, V, ld_w, d, target_c + r0, sums, nvt, part,
+                                   unit_m, z_y, e, ld_e, count, r0);
         });
         if (!grads) {
             hipLaunchKernelGGL((xent_rows_kernel<64, false>), dim3((unsigned)rows), dim3(64), 0,
-                               stream, part, z_y, nvt, V, target_c + r0, map + r0, terms, e, ld_e,
+                               stream, part, nullptr, z_y, nvt, V, target_c + r0, map + r0, terms, e, ld_e,
                                tok_loss, count, r0);
             continue;
         }
         hipLaunchKernelGGL((xent_rows_kernel<512, true>), dim3((unsigned)rows), dim3(512), 0, stream,
-                           part, z_y, nvt, V, target_c + r0, map + r0, terms, e, ld_e, tok_loss,
-                           count, r0);
+                           part, reinterpret_cast<const float*>(unit_m), z_y, nvt, V, target_c + r0,
+                           map + r0, terms, e, ld_e, tok_loss, count, r0);
         const dart_status_t st = lmhead::launch_bwd_gemms(
             e, ld_e, rows, V, w, ld_w, hr, d, d, parts && dh.p ? Grad{parts, d, false} : dh, false,
             parts ? P.ksplit : 1, P.rows * d, sum_w, P.acc_w && r0 > 0, stream, parts ? nullptr : map + r0,
