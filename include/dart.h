@@ -654,66 +654,64 @@ dart_status_t dart_grad_scale(void* x, dart_dtype_t dtype, int64_t rows, int64_t
 
 /* A quantised R x K matrix: every run of 32 values of a row (the last one of a
  * row may be shorter) is a block with one scale 2^e, its values q 2^e with q
- * one of 0, 0.5, 1, 1.5, 2, 3, 4, 6 or their negatives (E2M1), e from -127 to
- * 127 in one byte (E8M0; 255 stands for NaN). It lives in two device buffers
- * that the caller owns:
- *   packed: dart_mxfp4_packed_bytes(R, K) bytes, row-major, ceil(K/256) * 128
- *           bytes a row, value k of a row in the low (k even) or high four
- *           bits of byte k/2 (bit 3 the sign), zeros past K.
- *   scales: dart_mxfp4_scales_bytes(R, K) bytes: the scale byte of row r and
- *           block b at (((b/8) * ceil(R/32) + r/32) * 64 + (b%8)/4 * 32 + r%32) * 4
- *           + b%4; zeros for rows and blocks that do not exist.
- * Both 16-byte aligned. The functions below read nothing else of them.
- * Sizes in bytes, 0 for R or K outside [1, INT32_MAX]. Host only. */
-size_t dart_mxfp4_packed_bytes(int64_t R, int64_t K);
-size_t dart_mxfp4_scales_bytes(int64_t R, int64_t K);
+ * one of 0, 0.5, 1, 1.5, 2, 3, 4, 6 or their negatives (E2M1: bit 3 the sign), e from
+ * -127 to 127 in one byte e + 127 (E8M0; 255 stands for NaN). It lives in one device
+ * buffer of dart_mxfp4_bytes(R, K) bytes, 16-byte aligned, that the caller owns:
+ * ceil(R/32) x ceil(K/256) panels of 4352 bytes, row-major, zeros beyond the matrix. In the
+ * panel of rows r = 32 i + r' and columns k = 256 s + 32 b + j (b < 8, j < 32), value (r, k) is in
+ * the low (j even) or high four bits of byte
+ *   (b % 4) * 1024 + ((b / 4) * 32 + r') * 16 + j / 2,
+ * and its block's scale is byte 4096 + ((b / 4) * 32 + r') * 4 + b % 4: the order in which the
+ * matrix cores take them. Bytes of a buffer, 0 for R or K outside [1, INT32_MAX]. Host only. */
+size_t dart_mxfp4_bytes(int64_t R, int64_t K);
 
-/* Quantises x [R, ld >= K] (dtype fp32 or bf16): a block whose largest size is
+/* Quantises x [R, ld >= K] (dtype fp32 or bf16) to q: a block whose largest size is
  * a has e = max(floor(log2 a) - 2, -127) (-127 where a = 0) and each value's q
  * the nearest to value / 2^e, of two as near the one with an even code, sizes
  * beyond 6 taken as 6. A block with an infinity or a NaN stands for NaN
  * throughout (scale byte 255, values 0). Sums of products with such a block are NaN.
- * Errors: INVALID_ARG for a null or misaligned pointer (packed and scales 16
- * bytes, x one element), R or K outside [1, INT32_MAX], ld < K or an unknown
+ * Errors: INVALID_ARG for a null or misaligned pointer (q 16 bytes, x one
+ * element), R or K outside [1, INT32_MAX], ld < K or an unknown
  * dtype; UNSUPPORTED when ceil(R/32) * ceil(K/256) exceeds 2^24 - 1; HIP when
  * the launch fails. */
 dart_status_t dart_mxfp4_quantize(const void* x, dart_dtype_t dtype, int64_t R, int64_t K,
-                                  int64_t ld, void* packed, void* scales, hipStream_t stream);
+                                  int64_t ld, void* q, hipStream_t stream);
 
 /* The values that a quantised matrix stands for: out [R, ld_out >= K], fp32 or
  * bf16 (every one of dart_mxfp4_quantize's is exact in both). Columns [K, ld_out) are
  * not written. Errors as dart_mxfp4_quantize. */
-dart_status_t dart_mxfp4_dequantize(const void* packed, const void* scales, int64_t R, int64_t K,
-                                    dart_dtype_t dtype, void* out, int64_t ld_out,
-                                    hipStream_t stream);
+dart_status_t dart_mxfp4_dequantize(const void* q, int64_t R, int64_t K, dart_dtype_t dtype,
+                                    void* out, int64_t ld_out, hipStream_t stream);
 
 /* out = A B^T for quantised A [M, K] and B [N, K], on the matrix cores, summed
  * in fp32: the logits of tokens A under a head B kept in four bits.
  *   out: [M, ld_out >= N], fp32 or bf16 (round to nearest even); any alignment
  *        of whole elements. Columns [N, ld_out) are not written.
+ * The order of a sum, so its last bits, may differ between up to 32 rows of A and more.
  * Errors: INVALID_ARG for a null or misaligned pointer, a size outside
  * [1, INT32_MAX], ld_out < N or an unknown dtype; UNSUPPORTED when
- * ceil(M/256) * ceil(N/256) exceeds 8,388,607 or K 16,777,216; HIP when a
+ * ceil(M/256) * ceil(N/128) or ceil(N/32) exceeds 16,777,215 or K 16,777,216; HIP when a
  * launch fails. */
-dart_status_t dart_mxfp4_matmul(const void* a_packed, const void* a_scales, int64_t M,
-                                const void* b_packed, const void* b_scales, int64_t N, int64_t K,
+dart_status_t dart_mxfp4_matmul(const void* a, int64_t M, const void* b, int64_t N, int64_t K,
                                 dart_dtype_t dtype, void* out, int64_t ld_out, hipStream_t stream);
 
 /* dart_lmhead_tok_stats_ex for hidden states [T, d] and a weight [V, d] that
  * are quantised: log-probs, entropies and normalisers of a rollout policy whose
  * head is kept in four bits (the pi^Rollout of Sec. 4.4, whose difference from
  * the trainer's policy the truncated importance weight corrects), without
- * logits in memory. target, inv_temp, logp, entropy, lse, workspace (of
- * dart_lmhead_stats_workspace_bytes(T, V) bytes, 16-byte aligned) as there.
+ * logits in memory. target, inv_temp, logp, entropy, lse as there.
+ *   workspace: device memory of at least dart_lmhead_mxfp4_stats_workspace_bytes(T, V) bytes
+ *              (T * ceil(V/128) * 16 + T * 4), 16-byte aligned, owned by the
+ *              caller; contents on entry do not matter.
  * Errors: INVALID_ARG as dart_lmhead_tok_stats_ex and for a null or misaligned
- * buffer of a quantised matrix; UNSUPPORTED when ceil(T/256) * ceil(V/256) exceeds 8,388,607,
+ * quantised matrix; UNSUPPORTED when ceil(T/256) * ceil(V/128) exceeds 16,777,215,
  * T 67,108,860 or d 16,777,216; HIP when a launch fails. */
-dart_status_t dart_lmhead_mxfp4_tok_stats(const void* hidden_packed, const void* hidden_scales,
-                                          int64_t T, const void* weight_packed,
-                                          const void* weight_scales, int64_t V, int64_t d,
-                                          const int32_t* target, float inv_temp, float* logp,
-                                          float* entropy, float* lse, void* workspace,
-                                          size_t workspace_bytes, hipStream_t stream);
+dart_status_t dart_lmhead_mxfp4_tok_stats(const void* hidden, int64_t T, const void* weight,
+                                          int64_t V, int64_t d, const int32_t* target,
+                                          float inv_temp, float* logp, float* entropy, float* lse,
+                                          void* workspace, size_t workspace_bytes,
+                                          hipStream_t stream);
+size_t dart_lmhead_mxfp4_stats_workspace_bytes(int64_t T, int64_t V);
 
 /* Host helper (no device work): k = clamp(ceil(rho * S - 1e-6), 0, S), the
  * number of steps dart_step_select keeps (the guard absorbs the representation

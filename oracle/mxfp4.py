@@ -56,21 +56,18 @@ def quantize(x):
     return values, code, scale
 
 
-def packed_bytes(code):
-    """The packed buffer of a matrix's codes: two a byte, the even column low, rows padded with
-    zeros to 256 columns."""
+def buffer_bytes(code, scale):
+    """The buffer of a matrix's [R, K] codes and [R, blocks] scale bytes: panels of 32 rows x 256
+    columns, 4352 bytes each, zeros where there is nothing."""
     R, K = code.shape
-    full = np.zeros((R, -(-K // 256) * 256), np.uint8)
-    full[:, :K] = code
-    return full[:, 0::2] | full[:, 1::2] << 4
-
-
-def scale_bytes(scale):
-    """The scale buffer of a matrix's [R, blocks] scale bytes: per slice of 8 blocks and run of 32
-    rows 256 bytes, block b of row r at (b % 8 // 4) * 128 + r % 32 * 4 + b % 4; zeros elsewhere."""
-    R, nb = scale.shape
-    slices, runs = -(-nb // 8), -(-R // 32)
-    out = np.zeros((slices, runs, 256), np.uint8)
-    r, b = np.meshgrid(np.arange(R), np.arange(nb), indexing="ij")
-    out[b // 8, r // 32, b % 8 // 4 * 128 + r % 32 * 4 + b % 4] = scale
-    return out.reshape(-1)
+    runs, slices = -(-R // 32), -(-K // 256)
+    full = np.zeros((runs * 32, slices * 256), np.uint8)
+    full[:R, :K] = code
+    sc = np.zeros((runs * 32, slices * 8), np.uint8)
+    sc[:R, :scale.shape[1]] = scale
+    # [run, row, slice, half, ks, 16 pairs] -> [run, slice, ks, half, row, pair]
+    pairs = (full[:, 0::2] | full[:, 1::2] << 4).reshape(runs, 32, slices, 2, 4, 16)
+    values = pairs.transpose(0, 2, 4, 3, 1, 5).reshape(runs, slices, 4096)
+    # [run, row, slice, half, ks] -> [run, slice, half, row, ks]
+    scales = sc.reshape(runs, 32, slices, 2, 4).transpose(0, 2, 3, 1, 4).reshape(runs, slices, 256)
+    return np.concatenate([values, scales], 2).reshape(-1)

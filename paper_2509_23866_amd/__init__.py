@@ -54,8 +54,9 @@ EXPORTED = ("dart_tok_stats", "dart_step_select", "dart_tis_loss_fwd_bwd", "dart
             "dart_lmhead_backward_split_workspace_bytes",
             "dart_lmhead_xent_fwd", "dart_lmhead_xent_fwd_workspace_bytes",
             "dart_lmhead_xent_fwd_bwd", "dart_lmhead_xent_workspace_bytes", "dart_grad_scale",
-            "dart_mxfp4_packed_bytes", "dart_mxfp4_scales_bytes", "dart_mxfp4_quantize",
-            "dart_mxfp4_dequantize", "dart_mxfp4_matmul", "dart_lmhead_mxfp4_tok_stats",
+            "dart_mxfp4_bytes", "dart_mxfp4_quantize", "dart_mxfp4_dequantize",
+            "dart_mxfp4_matmul", "dart_lmhead_mxfp4_tok_stats",
+            "dart_lmhead_mxfp4_stats_workspace_bytes",
             "dart_kept_steps",
             "dart_status_string")
 
@@ -184,21 +185,19 @@ def load_library():
         lib.dart_lmhead_xent_workspace_bytes.argtypes = [_I64, _I64, _I64, _I64]
         lib.dart_grad_scale.restype = ctypes.c_int
         lib.dart_grad_scale.argtypes = [_P, ctypes.c_int, _I64, _I64, _I64, _P, _P]
-        lib.dart_mxfp4_packed_bytes.restype = ctypes.c_size_t
-        lib.dart_mxfp4_packed_bytes.argtypes = [_I64, _I64]
-        lib.dart_mxfp4_scales_bytes.restype = ctypes.c_size_t
-        lib.dart_mxfp4_scales_bytes.argtypes = [_I64, _I64]
+        lib.dart_mxfp4_bytes.restype = ctypes.c_size_t
+        lib.dart_mxfp4_bytes.argtypes = [_I64, _I64]
         lib.dart_mxfp4_quantize.restype = ctypes.c_int
-        lib.dart_mxfp4_quantize.argtypes = [_P, ctypes.c_int, _I64, _I64, _I64, _P, _P, _P]
+        lib.dart_mxfp4_quantize.argtypes = [_P, ctypes.c_int, _I64, _I64, _I64, _P, _P]
         lib.dart_mxfp4_dequantize.restype = ctypes.c_int
-        lib.dart_mxfp4_dequantize.argtypes = [_P, _P, _I64, _I64, ctypes.c_int, _P, _I64, _P]
+        lib.dart_mxfp4_dequantize.argtypes = [_P, _I64, _I64, ctypes.c_int, _P, _I64, _P]
         lib.dart_mxfp4_matmul.restype = ctypes.c_int
-        lib.dart_mxfp4_matmul.argtypes = [_P, _P, _I64, _P, _P, _I64, _I64, ctypes.c_int, _P, _I64,
-                                          _P]
+        lib.dart_mxfp4_matmul.argtypes = [_P, _I64, _P, _I64, _I64, ctypes.c_int, _P, _I64, _P]
         lib.dart_lmhead_mxfp4_tok_stats.restype = ctypes.c_int
-        lib.dart_lmhead_mxfp4_tok_stats.argtypes = [_P, _P, _I64, _P, _P, _I64, _I64, _P,
-                                                    ctypes.c_float, _P, _P, _P, _P,
-                                                    ctypes.c_size_t, _P]
+        lib.dart_lmhead_mxfp4_tok_stats.argtypes = [_P, _I64, _P, _I64, _I64, _P, ctypes.c_float, _P,
+                                                    _P, _P, _P, ctypes.c_size_t, _P]
+        lib.dart_lmhead_mxfp4_stats_workspace_bytes.restype = ctypes.c_size_t
+        lib.dart_lmhead_mxfp4_stats_workspace_bytes.argtypes = [_I64, _I64]
         lib.dart_kept_steps.restype = _I64
         lib.dart_kept_steps.argtypes = [_I64, ctypes.c_double]
         lib.dart_status_string.restype = ctypes.c_char_p
@@ -1090,35 +1089,33 @@ _FLOATS = {"torch.float32": DART_F32, "torch.bfloat16": DART_BF16}
 
 class Mxfp4(NamedTuple):
     """A rows x cols matrix in blocks of 32 four-bit values with a power-of-two scale, as
-    dart_mxfp4_quantize makes it: ``packed`` uint8 [rows, 128 ceil(cols / 256)], ``scales`` uint8
-    [dart_mxfp4_scales_bytes(rows, cols)] (include/dart.h says which byte is which)."""
+    dart_mxfp4_quantize makes it: ``data`` uint8 [dart_mxfp4_bytes(rows, cols)] (include/dart.h says
+    which byte is which)."""
 
-    packed: object
-    scales: object
+    data: object
     rows: int
     cols: int
 
 
-def dart_mxfp4_packed_bytes(R: int, K: int) -> int:
-    return int(load_library().dart_mxfp4_packed_bytes(int(R), int(K)))
+def dart_mxfp4_bytes(R: int, K: int) -> int:
+    return int(load_library().dart_mxfp4_bytes(int(R), int(K)))
 
 
-def dart_mxfp4_scales_bytes(R: int, K: int) -> int:
-    return int(load_library().dart_mxfp4_scales_bytes(int(R), int(K)))
+def dart_lmhead_mxfp4_stats_workspace_bytes(T: int, V: int) -> int:
+    return int(load_library().dart_lmhead_mxfp4_stats_workspace_bytes(int(T), int(V)))
 
 
 def _check_mxfp4(name, q, device=None):
     torch = _torch()
     if not isinstance(q, Mxfp4):
         raise TypeError(f"{name} must be an Mxfp4")
-    for part, t, n in (("packed", q.packed, dart_mxfp4_packed_bytes(q.rows, q.cols)),
-                       ("scales", q.scales, dart_mxfp4_scales_bytes(q.rows, q.cols))):
-        if (not isinstance(t, torch.Tensor) or t.dtype != torch.uint8 or not t.is_contiguous()
-                or n == 0 or t.numel() != n or not t.is_cuda or t.data_ptr() % 16):
-            raise ValueError(f"{name}.{part} must be a contiguous, 16-byte aligned uint8 tensor of "
-                             f"{n} bytes on a GPU")
-        if t.device != (q.packed.device if device is None else device):
-            raise ValueError(f"{name} must be on {q.packed.device if device is None else device}")
+    t, n = q.data, dart_mxfp4_bytes(q.rows, q.cols)
+    if (not isinstance(t, torch.Tensor) or t.dtype != torch.uint8 or not t.is_contiguous()
+            or n == 0 or t.numel() != n or not t.is_cuda or t.data_ptr() % 16):
+        raise ValueError(f"{name}.data must be a contiguous, 16-byte aligned uint8 tensor of {n} bytes "
+                         "on a GPU")
+    if device is not None and t.device != device:
+        raise ValueError(f"{name} must be on {device}")
 
 
 def dart_mxfp4_quantize(x, out=None, stream=None):
@@ -1136,15 +1133,13 @@ def dart_mxfp4_quantize(x, out=None, stream=None):
     if ld < K:
         raise ValueError("the rows of x must not overlap")
     if out is None:
-        packed = torch.empty((R, dart_mxfp4_packed_bytes(1, K)), dtype=torch.uint8, device=x.device)
-        scales = torch.empty(dart_mxfp4_scales_bytes(R, K), dtype=torch.uint8, device=x.device)
-        out = Mxfp4(packed, scales, R, K)
+        out = Mxfp4(torch.empty(dart_mxfp4_bytes(R, K), dtype=torch.uint8, device=x.device), R, K)
     else:
         _check_mxfp4("out", out, x.device)
         if (out.rows, out.cols) != (R, K):
             raise ValueError(f"out must be {R} x {K}")
     _enqueue("dart_mxfp4_quantize", x.device, stream, x.data_ptr(), _FLOATS[str(x.dtype)], R, K, ld,
-             out.packed.data_ptr(), out.scales.data_ptr())
+             out.data.data_ptr())
     return out
 
 
@@ -1155,9 +1150,9 @@ def dart_mxfp4_dequantize(q, dtype=None, out=None, stream=None):
     dtype = (torch.bfloat16 if out is None else out.dtype) if dtype is None else dtype
     if str(dtype) not in _FLOATS:
         raise TypeError("dtype must be float32 or bfloat16")
-    out = _out_matrix("out", out, (q.rows, q.cols), dtype, q.packed.device)
-    _enqueue("dart_mxfp4_dequantize", out.device, stream, q.packed.data_ptr(), q.scales.data_ptr(),
-             q.rows, q.cols, _FLOATS[str(dtype)], out.data_ptr(), _ld(out))
+    out = _out_matrix("out", out, (q.rows, q.cols), dtype, q.data.device)
+    _enqueue("dart_mxfp4_dequantize", out.device, stream, q.data.data_ptr(), q.rows,
+             q.cols, _FLOATS[str(dtype)], out.data_ptr(), _ld(out))
     return out
 
 
@@ -1167,7 +1162,7 @@ def _as_mxfp4(name, x, stream):
         _check_mxfp4(name, x)
         return x
     q = dart_mxfp4_quantize(x, stream=stream)
-    _used_on(stream, q.packed, q.scales)
+    _used_on(stream, q.data)
     return q
 
 
@@ -1180,15 +1175,14 @@ def dart_mxfp4_matmul(a, b, dtype=None, out=None, stream=None):
     dtype = (torch.bfloat16 if out is None else out.dtype) if dtype is None else dtype
     if str(dtype) not in _FLOATS:
         raise TypeError("dtype must be float32 or bfloat16")
-    dev = b.packed.device
+    dev = b.data.device
     cols = a.cols if isinstance(a, Mxfp4) else a.shape[-1]
-    if cols != b.cols or (a.packed if isinstance(a, Mxfp4) else a).device != dev:
+    if cols != b.cols or (a.data if isinstance(a, Mxfp4) else a).device != dev:
         raise ValueError("a and b must have the same inner size and be on one GPU")
     a = _as_mxfp4("a", a, stream)
     out = _out_matrix("out", out, (a.rows, b.rows), dtype, dev)
-    _enqueue("dart_mxfp4_matmul", dev, stream, a.packed.data_ptr(), a.scales.data_ptr(), a.rows,
-             b.packed.data_ptr(), b.scales.data_ptr(), b.rows, b.cols, _FLOATS[str(dtype)],
-             out.data_ptr(), _ld(out))
+    _enqueue("dart_mxfp4_matmul", dev, stream, a.data.data_ptr(), a.rows, b.data.data_ptr(), b.rows,
+             b.cols, _FLOATS[str(dtype)], out.data_ptr(), _ld(out))
     return out
 
 
@@ -1198,12 +1192,12 @@ def dart_lmhead_mxfp4_tok_stats(hidden, weight, target, inv_temp=1.0, logp=None,
     [V, d] and hidden states [T, d] in Mxfp4, or in float32 or bfloat16 and quantised first: the
     log-probs of a rollout policy whose head is kept in four bits, without materialising the logits.
     ``workspace``: "auto" (allocated here) or a uint8 device tensor of
-    dart_lmhead_stats_workspace_bytes(T, V) bytes."""
+    dart_lmhead_mxfp4_stats_workspace_bytes(T, V) bytes."""
     torch = _torch()
     _check_mxfp4("weight", weight)
-    dev = weight.packed.device
+    dev = weight.data.device
     cols = hidden.cols if isinstance(hidden, Mxfp4) else hidden.shape[-1]
-    if cols != weight.cols or (hidden.packed if isinstance(hidden, Mxfp4) else hidden).device != dev:
+    if cols != weight.cols or (hidden.data if isinstance(hidden, Mxfp4) else hidden).device != dev:
         raise ValueError("hidden and weight must have the same inner size d and be on one GPU")
     T, V = hidden.rows if isinstance(hidden, Mxfp4) else hidden.shape[0], weight.rows
     _check_vec("target", target, torch.int32, T, dev)
@@ -1212,11 +1206,10 @@ def dart_lmhead_mxfp4_tok_stats(hidden, weight, target, inv_temp=1.0, logp=None,
     lse = torch.empty(T, dtype=torch.float32, device=dev) if lse is None else lse
     for n, v in (("logp", logp), ("entropy", entropy), ("lse", lse)):
         _check_vec(n, v, torch.float32, T, dev)
-    workspace = _byte_workspace(workspace, dart_lmhead_stats_workspace_bytes(T, V), dev, stream)
+    workspace = _byte_workspace(workspace, dart_lmhead_mxfp4_stats_workspace_bytes(T, V), dev, stream)
     hidden = _as_mxfp4("hidden", hidden, stream)
-    _enqueue("dart_lmhead_mxfp4_tok_stats", dev, stream, hidden.packed.data_ptr(),
-             hidden.scales.data_ptr(), T, weight.packed.data_ptr(), weight.scales.data_ptr(), V,
-             weight.cols, target.data_ptr(), float(inv_temp), logp.data_ptr(), entropy.data_ptr(),
+    _enqueue("dart_lmhead_mxfp4_tok_stats", dev, stream, hidden.data.data_ptr(), T,
+             weight.data.data_ptr(), V, weight.cols, target.data_ptr(), float(inv_temp), logp.data_ptr(), entropy.data_ptr(),
              lse.data_ptr(), workspace.data_ptr(), workspace.numel())
     return logp, entropy, lse
 

@@ -731,7 +731,7 @@ dart_status_t launch_dlogits(const uint16_t* hidden, int64_t rows, int64_t d, in
     const int64_t nmt = (rows + LmCfg::BM - 1) / LmCfg::BM, nvt = vocab_tiles(V);
     if (!grid_fits(nmt * nvt, LmCfg::THREADS) || ld_h > kMaxLd || ld_w > kMaxLd)
         return DART_ERR_UNSUPPORTED;
-    with_tile<>(tile_rows(rows, V, d <= 1024 ? 57 : 54), rows, V, [&](auto cfg) {
+    with_tile(tile_rows(rows, V, d <= 1024 ? 57 : 54), rows, V, [&](auto cfg) {
         using C = decltype(cfg);
         const int64_t nm = (rows + C::BM - 1) / C::BM;
         hipLaunchKernelGGL(lmhead_dlogits_kernel<C>, dim3((unsigned)(nm * nvt)), dim3(C::THREADS),
@@ -772,7 +772,7 @@ dart_status_t dart_lmhead_tok_stats_ex(const void* hidden, int64_t T, int64_t d,
         return DART_ERR_UNSUPPORTED;
     float4* part = static_cast<float4*>(workspace);
     float* z_y = reinterpret_cast<float*>(part + T * nvt);
-    with_tile<>(tile_rows(T, V), T, V, [&](auto cfg) {
+    with_tile(tile_rows(T, V), T, V, [&](auto cfg) {
         using C = decltype(cfg);
         const int64_t nm = (T + C::BM - 1) / C::BM;
         hipLaunchKernelGGL(lmhead_stats_kernel<C>, dim3((unsigned)(nm * nvt)), dim3(C::THREADS), 0,

@@ -1,5 +1,5 @@
-// libdart internal: the MFMA tile that the LM-head kernels share, for bf16 and for
-// MXFP4 operands, and what their epilogues have in common.
+// libdart internal: the bf16 MFMA tile that the LM-head kernels share, and what their
+// epilogues have in common.
 #pragma once
 
 #include <hip/hip_runtime.h>
@@ -86,25 +86,8 @@ __device__ __forceinline__ int swz(int r) { return (r / (16 / CH)) % CH; }
 // Columns of a row that the statistics reduce together, in every configuration.
 constexpr int kStatsUnit = 64;
 
-// The K slices that are in flight or multiplied: BK elements of 16 bits per row,
-// chunk c of row r in slot c ^ swz(r).
-template <int NS, int BM, int BN, int BK>
-struct Slices {
-    uint16_t a[NS][BM][BK];
-    uint16_t b[NS][BN][BK];
-};
-// The same of MXFP4 operands (four values in 16 bits), with their scales: 64 dwords
-// for 32 rows, dword l the four scale bytes that lane l's MFMA operands have in the
-// slice. One load instruction brings those of 128 rows.
-template <int NS, int BM, int BN, int BK>
-struct ScaledSlices : Slices<NS, BM, BN, BK> {
-    uint32_t sa[NS][(BM < 128 ? 128 : BM) * 2];
-    uint32_t sb[NS][BN * 2];
-};
-
-template <int BM_, int BN_, int WM_, int WN_, int NS_, int BK_ = 64, bool SC_ = false>
+template <int BM_, int BN_, int WM_, int WN_, int NS_, int BK_ = 64>
 struct Cfg {
-    static constexpr bool SC = SC_;  // MXFP4 operands with scales, else bf16
     static constexpr int BM = BM_, BN = BN_, BK = BK_, WM = WM_, WN = WN_, NS = NS_;
     static_assert(NS == 2 || NS == 3, "buffers of the K loop");
     static constexpr int CH = BK / 8;          // 16-byte chunks per row and slice
@@ -128,8 +111,11 @@ struct Cfg {
     static_assert(THREADS % EPI == 0 || EPI % THREADS == 0, "epilogue rows");
     struct alignas(16) Smem {
         union {
-            typename std::conditional<SC, ScaledSlices<NS, BM, BN, BK>, Slices<NS, BM, BN, BK>>::type
-                in;
+            struct {
+                // slice buffers: BK bf16 per row, chunk c of row r in slot c ^ swz(r)
+                uint16_t a[NS][BM][BK];
+                uint16_t b[NS][BN][BK];
+            } in;
             float c[EPI][CROW];
             uint16_t c16[BM][CROW16];
             float4 red[BN / kStatsUnit][BM];  // per-row partial triples of the statistics
@@ -140,26 +126,17 @@ struct Cfg {
 // tiles, 4 or 8 waves, 2-4 buffers, 32- or 64-wide slices and register-staged
 // loads: 256 x 256 with 8 waves as 4 x 2 (64 x 128 per wave) and two 64-wide
 // buffers is the fastest.
-template <bool SC>
-using TileCfg = Cfg<256, 256, 4, 2, 2, 64, SC>;
-using LmCfg = TileCfg<false>;
+using LmCfg = Cfg<256, 256, 4, 2, 2>;
 // Tiles of fewer rows, for few rows in all: a third buffer fits the LDS, so that
 // two slices are in flight where W comes from HBM and little is multiplied per
 // byte of it. Measured (d = 3584, V = 152064; statistics and dlogits, us): 64
 // rows 213 and 204 with the 64-row tile (243 and 241 with two buffers), 279 and
 // 270 with the 256-row one; 128 rows 231 and 220 with the 128-row tile (274 and
 // 267 with two buffers), 285 and 281.
-template <bool SC>
-using TileCfg128 = Cfg<128, 256, 2, 4, 3, 64, SC>;
-template <bool SC>
-using TileCfg64 = Cfg<64, 256, 2, 4, 3, 64, SC>;
-using LmCfg128 = TileCfg128<false>;
-using LmCfg64 = TileCfg64<false>;
+using LmCfg128 = Cfg<128, 256, 2, 4, 3>;
+using LmCfg64 = Cfg<64, 256, 2, 4, 3>;
 static_assert(sizeof(LmCfg::Smem) <= 160 * 1024 && sizeof(LmCfg128::Smem) <= 160 * 1024 &&
-                  sizeof(LmCfg64::Smem) <= 160 * 1024 &&
-                  sizeof(TileCfg<true>::Smem) <= 160 * 1024 &&
-                  sizeof(TileCfg128<true>::Smem) <= 160 * 1024 &&
-                  sizeof(TileCfg64<true>::Smem) <= 160 * 1024,
+                  sizeof(LmCfg64::Smem) <= 160 * 1024,
               "LDS per workgroup");
 constexpr int kMergeWaves = 4;
 constexpr int kMergeBatch = 5;
@@ -198,34 +175,6 @@ __device__ __forceinline__ Triple merge(const Triple& a, const Triple& b) {
     return r;
 }
 
-// The scales of gemm_tile's operands: none, or an MXFP4 pair's (mxfp4.hip) with the
-// matrices' runs of 32 rows.
-struct NoScales {};
-struct Mxfp4Scales {
-    const uint32_t* a;
-    const uint32_t* b;
-    int64_t runs_a, runs_b;
-};
-
-// One 32 x 32 x 64 product of MXFP4 operands: byte ks of the scale dwords.
-[[maybe_unused]] __device__ __forceinline__ f32x16 mfma_mxfp4(int ks, u32x4 b, u32x4 a, f32x16 c,
-                                                              uint32_t sb, uint32_t sa) {
-#if defined(__HIP_DEVICE_COMPILE__)
-    typedef int i32x8 __attribute__((ext_vector_type(8)));
-    const i32x8 x = {(int)b[0], (int)b[1], (int)b[2], (int)b[3], 0, 0, 0, 0};
-    const i32x8 y = {(int)a[0], (int)a[1], (int)a[2], (int)a[3], 0, 0, 0, 0};
-    switch (ks) {  // the byte is part of the instruction; 4: both operands in E2M1
-        case 0: return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(x, y, c, 4, 4, 0, sb, 0, sa);
-        case 1: return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(x, y, c, 4, 4, 1, sb, 1, sa);
-        case 2: return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(x, y, c, 4, 4, 2, sb, 2, sa);
-        default: return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(x, y, c, 4, 4, 3, sb, 3, sa);
-    }
-#else
-    (void)ks, (void)b, (void)a, (void)sb, (void)sa;
-    return c;
-#endif
-}
-
 // acc = this wave's part of the tile A[m0:m0+BM, :] B[n0:n0+BN, :]^T (A [M, K]
 // and B [N, K] row-major bf16, rows 16-byte aligned, K % 8 == 0). Rows past M
 // or N read as zero (their results are not used); K past the end is zeroed in
@@ -240,22 +189,12 @@ struct Mxfp4Scales {
 // with bf16 gradients 10702 -> 10565 and 2953 -> 2856, dlogits 928 -> 917 at
 // 1000, the fp32 gradients within 0.3%.) Ends on a barrier with no loads in
 // flight, so the caller may reuse the LDS.
-//
-// MXFP4 operands (C::SC): A and B are then packed four-bit matrices seen as 16-bit
-// elements of four values (K, lda, ldb count those, K a multiple of BK), with the scales
-// that mxfp4.hip lays out. A slice is 256 values of a row, the same bytes as 64 bf16, and
-// an MFMA (v_mfma_scale_f32_32x32x64_f8f6f4, as many cycles as the bf16 one) takes two
-// 16-byte chunks of it, each one block of 32 values and its scale: lanes 0 - 31 chunk ks,
-// lanes 32 - 63 chunk 4 + ks, so that a lane's four scales of a slice are one dword. The
-// order of k within a slice is the same in A and B.
-template <class C, class S = NoScales>
+template <class C>
 __device__ __forceinline__ void gemm_tile(const uint16_t* __restrict__ A, int64_t M, int64_t lda,
                                           const uint16_t* __restrict__ B, int64_t N, int64_t ldb,
                                           int64_t K, int64_t m0, int64_t n0,
                                           typename C::Smem& sm,
-                                          f32x16 (&acc)[C::TM][C::TN],
-                                          [[maybe_unused]] const S& scales = S{}) {
-    static_assert(C::SC == std::is_same<S, Mxfp4Scales>::value, "scales of MXFP4 operands");
+                                          f32x16 (&acc)[C::TM][C::TN]) {
 #if defined(__HIP_DEVICE_COMPILE__)  // the gfx950 builtins below have no host form
     const int tid = threadIdx.x, lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);  // uniform: addresses in SGPRs
@@ -324,21 +263,6 @@ __device__ __forceinline__ void gemm_tile(const uint16_t* __restrict__ A, int64_
                 __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc_b, lds_ptr(lds_b(buf, q, hh)), 16,
                                                         voff_b, kb + q * qstride_b + hh * hstride_b,
                                                         0, 0);
-        if constexpr (C::SC) {
-            // the slice's scales, 128 rows an instruction: one of each issuing wave, the
-            // first two A's (the same one for tiles of up to 128 rows), the others B's; runs
-            // past the slice's last read as zero
-            static_assert(HW == 4 && C::BN == 256 && C::BM <= 256, "scale loads of the issuing waves");
-            const bool of_b = wave >= 2;
-            const int part = of_b || C::BM > 128 ? wave & 1 : 0;
-            const int64_t runs = of_b ? scales.runs_b : scales.runs_a;
-            const int64_t run = (of_b ? n0 : m0) / 32;
-            const uint32_t* src = (of_b ? scales.b : scales.a) + (kt * runs + run) * 64;
-            uint32_t* dst = (of_b ? sm.in.sb[buf] : sm.in.sa[buf]) + part * 256;
-            __builtin_amdgcn_raw_ptr_buffer_load_lds(tile_rsrc(src, (runs - run) * 256),
-                                                    lds_ptr(dst), 16, (uint32_t)lane * 16,
-                                                    (uint32_t)part * 1024, 0, 0);
-        }
     };
     // a partial last slice: zero the chunks past K
     auto zero_tail = [&](int64_t kt, int buf) {
@@ -367,8 +291,7 @@ __device__ __forceinline__ void gemm_tile(const uint16_t* __restrict__ A, int64_
     const uint32_t b_at = (uint32_t)(reinterpret_cast<const char*>(&sm.in.b[0][0][0]) - lds0);
 #pragma unroll
     for (int ks = 0; ks < C::KSTEPS; ++ks) {
-        const int c = C::SC ? (lane >> 5) * 4 + ks : ks * 2 + (lane >> 5);
-        const int ra = wr + (lane & 31), rb = wc + (lane & 31);
+        const int c = ks * 2 + (lane >> 5), ra = wr + (lane & 31), rb = wc + (lane & 31);
         rda[ks] = (uint32_t)(ra * BK + (c ^ swz<CH>(ra)) * 8) * 2;
         rdb[ks] = b_at + (uint32_t)(rb * BK + (c ^ swz<CH>(rb)) * 8) * 2;
         asm volatile("" : "+v"(rdb[ks]));
@@ -387,26 +310,6 @@ __device__ __forceinline__ void gemm_tile(const uint16_t* __restrict__ A, int64_
                 bf16x8, *reinterpret_cast<const u32x4*>(lds0 + rdb[ks] + buf * C::BN * BK * 2 +
                                                         j * 32 * BK * 2));
     };
-    // a slice's scale dwords of the lane's row and column blocks; their offsets opaque, so
-    // that block and buffer are immediates, as for B's operands
-    [[maybe_unused]] uint32_t sca[C::TM], scb[C::TN], rsa = 0, rsb = 0;
-    if constexpr (C::SC) {
-        rsa = (uint32_t)(reinterpret_cast<const char*>(&sm.in.sa[0][wr * 2 + lane]) - lds0);
-        rsb = (uint32_t)(reinterpret_cast<const char*>(&sm.in.sb[0][wc * 2 + lane]) - lds0);
-        asm volatile("" : "+v"(rsa), "+v"(rsb));
-    }
-    auto read_scales = [&](auto bufc) {
-        if constexpr (C::SC) {
-            constexpr int buf = decltype(bufc)::value;
-            auto at = [&](uint32_t off) { return *reinterpret_cast<const uint32_t*>(lds0 + off); };
-#pragma unroll
-            for (int i = 0; i < C::TM; ++i)
-                sca[i] = at(rsa + buf * (uint32_t)sizeof(sm.in.sa[0]) + i * C::RS * 8);
-#pragma unroll
-            for (int j = 0; j < C::TN; ++j)
-                scb[j] = at(rsb + buf * (uint32_t)sizeof(sm.in.sb[0]) + j * 32 * 8);
-        }
-    };
     // the MFMAs of row blocks [i0, i1) of k-step ks
     auto mfmas = [&](int ks, int i0 = 0, int i1 = C::TM) {
         const int set = ks & 1;
@@ -414,24 +317,17 @@ __device__ __forceinline__ void gemm_tile(const uint16_t* __restrict__ A, int64_
         for (int i = 0; i < C::TM; ++i)
 #pragma unroll
             for (int j = 0; j < C::TN; ++j)
-                if (i >= i0 && i < i1) {
-                    if constexpr (C::SC)
-                        acc[i][j] = mfma_mxfp4(ks, __builtin_bit_cast(u32x4, bfr[set][j]),
-                                               __builtin_bit_cast(u32x4, af[set][i]), acc[i][j],
-                                               scb[j], sca[i]);
-                    else
-                        acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(bfr[set][j], af[set][i],
-                                                                            acc[i][j], 0, 0, 0);
-                }
+                if (i >= i0 && i < i1)
+                    acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(bfr[set][j], af[set][i],
+                                                                        acc[i][j], 0, 0, 0);
     };
     // Every wave holds back the last k-step's MFMAs of its last row block
     // and issues them after the next slice's barrier (and its loads), while
     // the first operand reads of that slice are in flight.
     constexpr int LAST = C::KSTEPS - 1;
-    constexpr bool HELD = !C::SC;
 
     // NS LDS buffers: slices kt+1 .. kt+NS-1 load while slice kt is multiplied
-    constexpr int LOADS = 2 * (C::IA + C::IB) + C::SC;  // of an issuing wave and slice
+    constexpr int LOADS = 2 * (C::IA + C::IB);  // of an issuing wave and slice
     auto slice = [&](auto bufc, int64_t kt) {
         constexpr int buf = decltype(bufc)::value;
         // slice kt has landed for this wave; the barrier makes it so for all,
@@ -441,7 +337,7 @@ __device__ __forceinline__ void gemm_tile(const uint16_t* __restrict__ A, int64_
         else
             wait_vmcnt<(C::NS - 2) * LOADS>();
         lds_ring_barrier();
-        if (!C::SC && (K % BK) && kt == nk - 1) {
+        if ((K % BK) && kt == nk - 1) {
             zero_tail(kt, buf);
             lds_ring_barrier();
         }
@@ -449,14 +345,12 @@ __device__ __forceinline__ void gemm_tile(const uint16_t* __restrict__ A, int64_
         // the operands of k-step ks+1 are read while the MFMAs of k-step ks issue
         read_step(bufc, 0, 0);
         __builtin_amdgcn_s_setprio(1);
-        if (HELD && kt > 0) mfmas(LAST, C::TM - 1, C::TM);
-        read_scales(bufc);
-        if constexpr (C::SC) __builtin_amdgcn_sched_barrier(0);
+        if (kt > 0) mfmas(LAST, C::TM - 1, C::TM);
 #pragma unroll
         for (int ks = 0; ks < C::KSTEPS; ++ks) {
             const int cs = ks & 1;
             if (ks < C::KSTEPS - 1) read_step(bufc, ks + 1, cs ^ 1);
-            mfmas(ks, 0, HELD && ks == C::KSTEPS - 1 ? C::TM - 1 : C::TM);
+            mfmas(ks, 0, ks == C::KSTEPS - 1 ? C::TM - 1 : C::TM);
             if (ks < C::KSTEPS - 1) {
                 // interleave: one LDS read, then a share of the MFMAs
 #pragma unroll
@@ -465,7 +359,6 @@ __device__ __forceinline__ void gemm_tile(const uint16_t* __restrict__ A, int64_
                     __builtin_amdgcn_sched_group_barrier(0x008, (C::TM * C::TN) / (C::TM + C::TN), 0);
                 }
             }
-            if constexpr (C::SC) __builtin_amdgcn_sched_barrier(0);
         }
         __builtin_amdgcn_s_setprio(0);
     };
@@ -483,7 +376,7 @@ __device__ __forceinline__ void gemm_tile(const uint16_t* __restrict__ A, int64_
     }
     if (kt < nk) slice(std::integral_constant<int, 0>{}, kt);
     if (C::NS > 2 && kt + 1 < nk) slice(std::integral_constant<int, 1>{}, kt + 1);
-    if (HELD) mfmas(LAST, C::TM - 1, C::TM);
+    mfmas(LAST, C::TM - 1, C::TM);
     __syncthreads();
 #else
     (void)A, (void)M, (void)lda, (void)B, (void)N, (void)ldb, (void)K, (void)m0, (void)n0;
@@ -541,8 +434,7 @@ __device__ __forceinline__ void tile_of_block(int64_t nmt, int64_t nvt, int64_t&
 __host__ __device__ constexpr bool has_rest(int64_t nmt) { return nmt == 3 || nmt == 4; }
 template <class C>
 struct Rest {
-    using type =
-        typename std::conditional<C::BM == LmCfg::BM, TileCfg128<C::SC>, C>::type;
+    using type = typename std::conditional<C::BM == LmCfg::BM, LmCfg128, C>::type;
 };
 // f(configuration, LDS, first row, vocabulary tile) for this workgroup's tile of M
 // rows x nvt vocabulary tiles, if it has one; with X also an X in LDS as f's last
@@ -798,15 +690,15 @@ inline int tile_rows(int64_t rows, int64_t V, double t128 = 54) {
 
 // f(configuration of bm-row tiles) for rows x V logits. The launch's limits are checked
 // with 256-row tiles, as ever; smaller ones are taken where they fit too.
-template <bool SC = false, class F>
+template <class F>
 void with_tile(int bm, int64_t rows, int64_t V, F&& f) {
     if (!grid_fits((rows + bm - 1) / bm * vocab_tiles(V), LmCfg::THREADS)) bm = 256;
     if (bm == 64)
-        f(TileCfg64<SC>{});
+        f(LmCfg64{});
     else if (bm == 128)
-        f(TileCfg128<SC>{});
+        f(LmCfg128{});
     else
-        f(TileCfg<SC>{});
+        f(LmCfg{});
 }
 
 }  // namespace

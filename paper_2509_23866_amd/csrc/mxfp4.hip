@@ -6,35 +6,47 @@
 // a rollout policy that differs from the trainer's by quantisation; this part makes that
 // policy's head (quantise), its logits (product) and its log-probs (statistics).
 //
-//   mxfp4_quantize_kernel    one workgroup per 32 rows x 256 columns: four lanes a block,
-//                            their largest size by two exchanges, E2M1 by the hardware's
-//                            conversion. Bound by memory.
-//   mxfp4_dequantize_kernel  the same tile back.
-//   mxfp4_matmul_kernel      gemm_tile on MXFP4 operands, the fp32 tile written in bf16 or
-//                            fp32.
-//   mxfp4_stats_kernel       gemm_tile and the epilogue of lmhead_stats_kernel: the
+//   mxfp4_quantize_kernel    one workgroup per panel: four lanes a block, their largest
+//                            size by two exchanges, E2M1 by the hardware's conversion.
+//                            Bound by memory.
+//   mxfp4_dequantize_kernel  a panel back.
+//   mxfp4_few_kernel         the product of up to 32 rows: a workgroup per 32 rows of B, its
+//                            four waves on different panels of them, joined in LDS.
+//                            Bound by B's bytes.
+//   mxfp4_matmul_kernel      the product of more rows: mxfp4_tile, the fp32 tile written
+//                            in bf16 or fp32.
+//   mxfp4_stats_kernel       mxfp4_tile and the epilogue of lmhead_stats_kernel: the
 //                            logits are not written.
 //
-// Layout of a quantised R x K matrix, in slices of 256 columns (K padded with zeros to
-// whole slices) and runs of 32 rows:
-//   packed  row-major, slices * 128 bytes a row, value k in the low (k even) or high half
-//           of byte k / 2;
-//   scales  [slice][run][64] dwords: byte ks of dword half * 32 + r is the scale of block
-//           half * 4 + ks (of the slice's 8) of row r (of the run's 32). So one dword holds
-//           the scales of a lane's four MFMA operands in a slice, 64 lanes read 256 bytes in
-//           a row, and one load instruction brings those of 128 rows.
+// Layout of a quantised R x K matrix: panels of 32 rows x 256 columns, padded with zeros at
+// the matrix's edges, [ceil(R / 32)][ceil(K / 256)], each the operands of four
+// v_mfma_scale_f32_32x32x64_f8f6f4 as a wave holds them:
+//   bytes ks * 1024 + l * 16 ..  (ks < 4, l < 64): lane l's operand of product ks, the block
+//                               (l / 32) * 4 + ks of row l % 32, value j in the low (j even)
+//                               or high half of byte j / 2;
+//   bytes 4096 + l * 4 + ks     its scale.
+// So a lane's four operands have their scales in one dword, a wave reads an operand as 1 KB
+// in a row, from memory or from LDS, without a bank conflict, and no edge needs a check.
 #include "lmhead_tile.h"
 
 namespace {
 
-constexpr int64_t kSlice = 256;  // columns
-constexpr int64_t kRun = 32;     // rows
+constexpr int64_t kSlice = 256;  // columns of a panel
+constexpr int64_t kRun = 32;     // rows of a panel
+constexpr uint32_t kPanel = 4352, kScalesAt = 4096;  // bytes
 constexpr int kQuantThreads = 256;
 
 int64_t slices_of(int64_t K) { return (K + kSlice - 1) / kSlice; }
 int64_t runs_of(int64_t R) { return (R + kRun - 1) / kRun; }
-// a packed row in 16-bit elements
-int64_t packed_ld(int64_t K) { return slices_of(K) * (kSlice / 4); }
+
+// Where values [8 c8, 8 c8 + 8) of row r of a panel are (four bytes), and their block's scale.
+__device__ __forceinline__ uint32_t value_at(int r, int c8) {
+    const int b = c8 >> 2;
+    return (uint32_t)((b & 3) * 1024 + ((b >> 2) * 32 + r) * 16 + (c8 & 3) * 4);
+}
+__device__ __forceinline__ uint32_t scale_at(int r, int b) {
+    return kScalesAt + (uint32_t)(((b >> 2) * 32 + r) * 4 + (b & 3));
+}
 
 // x of the lane that differs in bit 0 (B = 1) or 1 (B = 2) of its number.
 template <int B>
@@ -64,6 +76,7 @@ __device__ __forceinline__ uint32_t e2m1x8(const float (&v)[8]) {
 // The hardware takes 16-byte vectors at any multiple of an element's size.
 typedef u32x4 __attribute__((aligned(2))) u32x4_at2;
 typedef u32x4 __attribute__((aligned(4))) u32x4_at4;
+typedef u32x2 __attribute__((aligned(2))) u32x2_at2;
 
 // Eight values of a row, the first `left` of them, then zeros.
 __device__ __forceinline__ void load8(const float* p, int64_t left, float (&v)[8]) {
@@ -101,10 +114,9 @@ __device__ __forceinline__ uint32_t scale_byte(uint32_t top) {
 
 template <class X>
 __global__ void __launch_bounds__(kQuantThreads)
-mxfp4_quantize_kernel(const X* __restrict__ x, int64_t R, int64_t K, int64_t ld,
-                      int64_t slices, int64_t runs, uint8_t* __restrict__ packed,
-                      uint32_t* __restrict__ scales) {
-    __shared__ uint32_t sc[64];
+mxfp4_quantize_kernel(const X* __restrict__ x, int64_t R, int64_t K, int64_t ld, int64_t slices,
+                      uint8_t* __restrict__ out) {
+    __shared__ alignas(16) uint8_t panel[kPanel];
     const int64_t run = blockIdx.x / slices, slice = blockIdx.x % slices;
     const int tid = threadIdx.x, c8 = tid & 31;
     const int64_t k = slice * kSlice + c8 * 8;
@@ -117,7 +129,6 @@ mxfp4_quantize_kernel(const X* __restrict__ x, int64_t R, int64_t K, int64_t ld,
 #pragma unroll
     for (int p = 0; p < 4; ++p) {
         const int row = p * 8 + (tid >> 5);
-        const int64_t r = run * kRun + row;
         uint32_t top = 0;
 #pragma unroll
         for (int i = 0; i < 8; ++i) top = max(top, __float_as_uint(v[p][i]) & 0x7FFFFFFFu);
@@ -128,15 +139,15 @@ mxfp4_quantize_kernel(const X* __restrict__ x, int64_t R, int64_t K, int64_t ld,
         const float inv = __uint_as_float((254u - min(byte, 252u)) << 23);
 #pragma unroll
         for (int i = 0; i < 8; ++i) v[p][i] *= inv;
-        const uint32_t w = byte == 255u ? 0u : e2m1x8(v[p]);
-        if (r < R)
-            *reinterpret_cast<uint32_t*>(packed + (r * slices + slice) * 128 + c8 * 4) = w;
-        const int c = c8 >> 2;
-        if ((c8 & 3) == 0)
-            reinterpret_cast<uint8_t*>(sc)[(c >> 2) * 128 + row * 4 + (c & 3)] = (uint8_t)byte;
+        *reinterpret_cast<uint32_t*>(panel + value_at(row, c8)) = byte == 255u ? 0u : e2m1x8(v[p]);
+        if ((c8 & 3) == 0) panel[scale_at(row, c8 >> 2)] = (uint8_t)byte;
     }
     __syncthreads();
-    if (tid < 64) scales[(slice * runs + run) * 64 + tid] = sc[tid];
+    u32x4* dst = reinterpret_cast<u32x4*>(out + (int64_t)blockIdx.x * kPanel);
+    const u32x4* src = reinterpret_cast<const u32x4*>(panel);
+    dst[tid] = src[tid];
+    static_assert(kPanel / 16 - kQuantThreads == 16, "the scales: sixteen more vectors");
+    if (tid < 16) dst[kQuantThreads + tid] = src[kQuantThreads + tid];
 }
 
 // Up to eight results at p, the first `left` of them.
@@ -162,35 +173,35 @@ __device__ __forceinline__ void store8(uint16_t* p, int64_t left, const float (&
 
 template <class X>
 __global__ void __launch_bounds__(kQuantThreads)
-mxfp4_dequantize_kernel(const uint8_t* __restrict__ packed, const uint8_t* __restrict__ scales,
-                        int64_t R, int64_t K, int64_t slices, int64_t runs,
+mxfp4_dequantize_kernel(const uint8_t* __restrict__ q, int64_t R, int64_t K, int64_t slices,
                         X* __restrict__ out, int64_t ld) {
+    __shared__ alignas(16) uint8_t panel[kPanel];
     const int64_t run = blockIdx.x / slices, slice = blockIdx.x % slices;
-    const int tid = threadIdx.x, c8 = tid & 31, c = c8 >> 2;
+    const int tid = threadIdx.x, c8 = tid & 31;
+    const u32x4* src = reinterpret_cast<const u32x4*>(q + (int64_t)blockIdx.x * kPanel);
+    u32x4* dst = reinterpret_cast<u32x4*>(panel);
+    dst[tid] = src[tid];
+    if (tid < 16) dst[kQuantThreads + tid] = src[kQuantThreads + tid];
+    __syncthreads();
     const int64_t k = slice * kSlice + c8 * 8;
     if (k >= K) return;
-    uint32_t w[4], byte[4];
 #pragma unroll
     for (int p = 0; p < 4; ++p) {
         const int row = p * 8 + (tid >> 5);
-        const int64_t r = min(run * kRun + row, R - 1);
-        w[p] = *reinterpret_cast<const uint32_t*>(packed + (r * slices + slice) * 128 + c8 * 4);
-        byte[p] = scales[(slice * runs + run) * 256 + (c >> 2) * 128 + row * 4 + (c & 3)];
-    }
-#pragma unroll
-    for (int p = 0; p < 4; ++p) {
-        const int64_t r = run * kRun + p * 8 + (tid >> 5);
+        const int64_t r = run * kRun + row;
         if (r >= R) return;
+        const uint32_t w = *reinterpret_cast<const uint32_t*>(panel + value_at(row, c8));
+        const uint32_t byte = panel[scale_at(row, c8 >> 2)];
         // the scale as fp32 (2^-127 is a denormal, byte 255 a NaN); a code's three bits
         // below the sign as the low exponent and high mantissa bits of an fp32, times
         // 2^126, are its size (0.5 from the denormal 2^-127)
-        const float scale = byte[p] == 255u   ? __builtin_nanf("")
-                            : byte[p] == 0u   ? __uint_as_float(0x00400000u)
-                                              : __uint_as_float(byte[p] << 23);
+        const float scale = byte == 255u ? __builtin_nanf("")
+                            : byte == 0u ? __uint_as_float(0x00400000u)
+                                         : __uint_as_float(byte << 23);
         float v[8];
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-            const uint32_t code = w[p] >> (4 * i);
+            const uint32_t code = w >> (4 * i);
             const float size = __uint_as_float((code & 7u) << 22) * 0x1p126f;
             v[i] = __uint_as_float(__float_as_uint(size) | (code & 8u) << 28) * scale;
         }
@@ -198,16 +209,238 @@ mxfp4_dequantize_kernel(const uint8_t* __restrict__ packed, const uint8_t* __res
     }
 }
 
+// One 32 x 32 x 64 product of MXFP4 operands: byte ks of the scale dwords.
+__device__ __forceinline__ f32x16 mfma_mxfp4(int ks, u32x4 b, u32x4 a, f32x16 c, uint32_t sb,
+                                             uint32_t sa) {
+#if defined(__HIP_DEVICE_COMPILE__)
+    typedef int i32x8 __attribute__((ext_vector_type(8)));
+    const i32x8 x = {(int)b[0], (int)b[1], (int)b[2], (int)b[3], 0, 0, 0, 0};
+    const i32x8 y = {(int)a[0], (int)a[1], (int)a[2], (int)a[3], 0, 0, 0, 0};
+    switch (ks) {  // the byte is part of the instruction; 4: both operands in E2M1
+        case 0: return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(x, y, c, 4, 4, 0, sb, 0, sa);
+        case 1: return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(x, y, c, 4, 4, 1, sb, 1, sa);
+        case 2: return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(x, y, c, 4, 4, 2, sb, 2, sa);
+        default: return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(x, y, c, 4, 4, 3, sb, 3, sa);
+    }
+#else
+    (void)ks, (void)b, (void)a, (void)sb, (void)sa;
+    return c;
+#endif
+}
+
+// A lane's vector (or dword) at a byte offset of a run of panels, the slice's part of the
+// offset in a scalar.
+__device__ __forceinline__ u32x4 load_operand(__amdgpu_buffer_rsrc_t r, uint32_t lane_at,
+                                              uint32_t wave_at) {
+#if defined(__HIP_DEVICE_COMPILE__)
+    return __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(r, lane_at, wave_at, 0));
+#else
+    (void)r, (void)lane_at, (void)wave_at;
+    return u32x4{0u, 0u, 0u, 0u};
+#endif
+}
+__device__ __forceinline__ uint32_t load_scales(__amdgpu_buffer_rsrc_t r, uint32_t lane_at,
+                                                uint32_t wave_at) {
+#if defined(__HIP_DEVICE_COMPILE__)
+    return __builtin_amdgcn_raw_buffer_load_b32(r, lane_at, wave_at, 0);
+#else
+    (void)r, (void)lane_at, (void)wave_at;
+    return 0u;
+#endif
+}
+
+// Tile configuration: BM rows of A x 128 of B per workgroup of four waves, WM x WN, each
+// owning (BM / WM) x (128 / WN) as 32 x 32 MFMA tiles; K in slices of 256, one panel of every
+// 32 rows. A wave's panels of A go from memory (L2) to registers, those of B to an LDS ring of
+// NS slices, from which the waves share them: an operand byte read from LDS serves one
+// product, and with both operands there (the bf16 tile's way) the LDS was the limit. Two
+// workgroups run per compute unit, so that one multiplies while the other is in its epilogue.
+// TILETIMES
+template <int BM_, int WM_, int WN_, int NS_>
+struct Cfg4 {
+    static constexpr int BM = BM_, BN = 128, WM = WM_, WN = WN_, NS = NS_;
+    static constexpr int WAVES = 4, THREADS = 256;
+    static constexpr int TM = BM / WM / 32, TN = BN / WN / 32;  // MFMA tiles per wave
+    static constexpr int SETS = TM == 1 ? 2 : 1;  // of registers for A's panels
+    static constexpr int RS = WM * 32;  // rows between a wave's row blocks
+    static constexpr int RUNS = BN / 32;  // panels of B a slice: one for each wave to bring
+    static constexpr int CROW = BN + 4, CROW16 = BN + 8;  // as in Cfg
+    static_assert(WM * WN == WAVES && RUNS == WAVES && TM * WM * 32 == BM && TN * WN * 32 == BN,
+                  "four waves");
+    static_assert(SETS == 1 || NS % 2 == 0, "a slice's set goes by its buffer");
+    struct alignas(16) Smem {
+        union {
+            uint8_t b[NS][RUNS][kPanel];
+            float c[RS][CROW];
+            uint16_t c16[BM][CROW16];
+            float4 red[BN / kStatsUnit][BM];
+        };
+    };
+    static_assert(sizeof(Smem) <= 80 * 1024, "two workgroups per compute unit");
+};
+// 256 rows; fewer for few rows, with more slices in flight where B comes from HBM and little
+// is multiplied per byte of it.
+using Mx256 = Cfg4<256, 4, 1, 3>;
+using Mx128 = Cfg4<128, 4, 1, 4>;
+using Mx64 = Cfg4<64, 2, 2, 4>;
+
+// The operands of a product: panels, and panels per row of panels.
+struct Mxfp4Pair {
+    const uint8_t *a, *b;
+    int64_t runs_a, runs_b, slices;
+};
+
+// acc = this wave's part of the tile of A's rows [m0, m0 + BM) x B's rows [n0, n0 + 128) of
+// A B^T; rows past the matrices' last panels read as zero. Layout of acc as gemm_tile's. Ends on
+// a barrier with no loads in flight, so the caller may reuse the LDS.
+template <class C>
+__device__ __forceinline__ void mxfp4_tile(const Mxfp4Pair& x, int64_t m0, int64_t n0,
+                                           typename C::Smem& sm, f32x16 (&acc)[C::TM][C::TN]) {
+#if defined(__HIP_DEVICE_COMPILE__)
+    const int tid = threadIdx.x, lane = tid & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+#pragma unroll
+    for (int i = 0; i < C::TM; ++i)
+#pragma unroll
+        for (int j = 0; j < C::TN; ++j)
+#pragma unroll
+            for (int v = 0; v < 16; ++v) acc[i][j][v] = 0.f;
+
+    // a run of panels is a resource of its own, so that loads past its last slice read as zero
+    // without going to memory: the loop below needs no condition on them
+    const int64_t nk = x.slices, run_bytes = nk * kPanel;
+    auto run_rsrc = [&](const uint8_t* p, int64_t run, int64_t runs) {
+        return tile_rsrc(p + (run < runs ? run : 0) * run_bytes, run < runs ? run_bytes : 0);
+    };
+    __amdgpu_buffer_rsrc_t ra[C::TM];
+#pragma unroll
+    for (int i = 0; i < C::TM; ++i)
+        ra[i] = run_rsrc(x.a, m0 / kRun + wave / C::WN + i * C::WM, x.runs_a);
+    const __amdgpu_buffer_rsrc_t rb = run_rsrc(x.b, n0 / kRun + wave, x.runs_b);
+    const uint32_t l16 = (uint32_t)lane * 16, l4 = (uint32_t)lane * 4, s4 = kScalesAt + l4;
+
+    // slice kt's panels of B into buffer buf: every wave one run, four operands and the scales
+    auto issue = [&](int64_t kt, int buf) {
+        const uint32_t at = (uint32_t)kt * kPanel;
+        uint8_t* dst = &sm.b[buf][wave][0];
+#pragma unroll
+        for (uint32_t ks = 0; ks < 4; ++ks)
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(rb, lds_ptr(dst + ks * 1024), 16, l16,
+                                                    at + ks * 1024, 0, 0);
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(rb, lds_ptr(dst + kScalesAt), 4, l4, at + kScalesAt,
+                                                0, 0);
+    };
+    u32x4 af[C::SETS][4][C::TM];
+    uint32_t sa[C::TM], sa_next[C::TM], sb[C::TN];
+    auto load_a = [&](int64_t kt, int ks, int a_set) {
+#pragma unroll
+        for (int i = 0; i < C::TM; ++i)
+            af[a_set][ks][i] = load_operand(ra[i], l16, (uint32_t)kt * kPanel + (uint32_t)ks * 1024);
+    };
+    auto load_sa = [&](int64_t kt) {
+#pragma unroll
+        for (int i = 0; i < C::TM; ++i)
+            sa_next[i] = load_scales(ra[i], s4, (uint32_t)kt * kPanel);
+    };
+    // the wave's first column block; opaque, so that buffer, block and product are the
+    // reads' immediates
+    uint32_t rd = (uint32_t)((wave % C::WN) * C::TN) * kPanel + l16;
+    uint32_t rs = (uint32_t)((wave % C::WN) * C::TN) * kPanel + s4;
+    asm volatile("" : "+v"(rd), "+v"(rs));
+    const char* const lds0 = reinterpret_cast<const char*>(&sm);
+    u32x4 bf[2][C::TN];
+    auto read_b = [&](auto bufc, int ks, int set) {
+        constexpr uint32_t buf = decltype(bufc)::value;
+#pragma unroll
+        for (uint32_t j = 0; j < C::TN; ++j)
+            bf[set][j] = *reinterpret_cast<const u32x4*>(lds0 + rd + (buf * C::RUNS + j) * kPanel +
+                                                         ks * 1024);
+    };
+    // When slice kt begins, the loads of B's slices kt + 1 .. kt + NS - 2, five each, were issued
+    // after those of kt; waiting until no more than so many loads are left has slice kt landed,
+    // wherever the compiler put A's.
+    constexpr int AHEAD = 5 * (C::NS - 2);
+    auto slice = [&](auto bufc, int64_t kt) {
+        constexpr int buf = decltype(bufc)::value;
+        wait_vmcnt<AHEAD>();
+        lds_ring_barrier();
+        // A's next slice: with two sets of registers now, before the loads of B, which may then
+        // stay in flight when it is waited for; with one as the products let go of it
+        constexpr int set_a = C::SETS == 2 ? buf & 1 : 0;
+        if constexpr (C::SETS == 2) {
+#pragma unroll
+            for (int i = 0; i < C::TM; ++i) sa[i] = sa_next[i];
+            load_sa(kt + 1);
+#pragma unroll
+            for (int ks = 0; ks < 4; ++ks) load_a(kt + 1, ks, set_a ^ 1);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        issue(kt + C::NS - 1, (buf + C::NS - 1) % C::NS);
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (uint32_t j = 0; j < C::TN; ++j)
+            sb[j] = *reinterpret_cast<const uint32_t*>(lds0 + rs + (buf * C::RUNS + j) * kPanel);
+        read_b(bufc, 0, 0);
+        if constexpr (C::SETS == 1) {
+#pragma unroll
+            for (int i = 0; i < C::TM; ++i) sa[i] = sa_next[i];
+            load_sa(kt + 1);
+        }
+        __builtin_amdgcn_sched_barrier(0);
+        __builtin_amdgcn_s_setprio(1);
+#pragma unroll
+        for (int ks = 0; ks < 4; ++ks) {
+            const int set = ks & 1;
+            if (ks < 3) read_b(bufc, ks + 1, set ^ 1);
+#pragma unroll
+            for (int i = 0; i < C::TM; ++i)
+#pragma unroll
+                for (int j = 0; j < C::TN; ++j)
+                    acc[i][j] = mfma_mxfp4(ks, bf[set][j], af[set_a][ks][i], acc[i][j], sb[j], sa[i]);
+            if constexpr (C::SETS == 1) load_a(kt + 1, ks, 0);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        __builtin_amdgcn_s_setprio(0);
+        // the products stay in their slice (the compiler moved them to the next branch, with
+        // every operand on the way in registers)
+#pragma unroll
+        for (int i = 0; i < C::TM; ++i)
+#pragma unroll
+            for (int j = 0; j < C::TN; ++j) asm volatile("" : "+v"(acc[i][j]));
+    };
+    load_sa(0);
+#pragma unroll
+    for (int ks = 0; ks < 4; ++ks) load_a(0, ks, 0);
+    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int b = 0; b < C::NS - 1; ++b) issue(b, b);
+    int64_t kt = 0;
+    for (; kt + C::NS - 1 < nk; kt += C::NS) {
+        slice(std::integral_constant<int, 0>{}, kt);
+        slice(std::integral_constant<int, 1>{}, kt + 1);
+        slice(std::integral_constant<int, 2>{}, kt + 2);
+        if constexpr (C::NS > 3) slice(std::integral_constant<int, 3 % C::NS>{}, kt + 3);
+    }
+    if (kt < nk) slice(std::integral_constant<int, 0>{}, kt);
+    if (kt + 1 < nk) slice(std::integral_constant<int, 1>{}, kt + 1);
+    if (C::NS > 3 && kt + 2 < nk) slice(std::integral_constant<int, 2>{}, kt + 2);
+    static_assert(C::NS == 3 || C::NS == 4, "buffers of the K loop");
+    wait_vmcnt<0>();  // the zeros of slices past the last are in LDS
+    __syncthreads();
+#else
+    (void)x, (void)m0, (void)n0, (void)sm, (void)acc;
+#endif
+}
+
 // This wave's part of a result tile to out [M, ld] through the wave's own part of the
 // LDS (its accesses run in order: no barrier), 32 rows at a time, as in
-// lmhead_dlogits_tile: bf16 rows of the wave's columns, fp32 ones 64 columns at a time, in
-// 16-byte vectors, which the hardware takes at any multiple of an element's size.
+// lmhead_dlogits_tile: bf16 rows of the wave's columns, fp32 ones 64 columns at a time.
 template <class C, class O>
 __device__ __forceinline__ void store_tile(f32x16 (&acc)[C::TM][C::TN], int64_t M, int64_t N,
                                            O* __restrict__ out, int64_t ld, typename C::Smem& sm,
                                            int64_t m0, int64_t n0) {
     constexpr bool BF16 = sizeof(O) == 2;
-    constexpr int NJ = BF16 ? C::TN : 2;                        // 32-column blocks a piece
+    constexpr int NJ = BF16 ? C::TN : 2;  // 32-column blocks a piece
     constexpr int EPC = 16 / sizeof(O), CPR = NJ * 32 / EPC, RPI = 64 / CPR;
     using vec_t = typename std::conditional<BF16, u32x4_at2, u32x4_at4>::type;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
@@ -251,81 +484,153 @@ __device__ __forceinline__ void store_tile(f32x16 (&acc)[C::TM][C::TN], int64_t 
         }
 }
 
-// The operands of a product: packed matrices and their scales.
-struct Mxfp4Pair {
-    const uint16_t *a, *b;
-    Mxfp4Scales scales;
-    int64_t K4;  // columns in 16-bit elements: the row stride too
-};
+// f(LDS, first row, column tile) for this workgroup's tile of M rows x nnt column tiles.
+template <class C, class F>
+__device__ __forceinline__ void with_mxfp4_tile(int64_t M, int64_t nnt, F&& f) {
+    __shared__ typename C::Smem sm;
+    int64_t mt, nt;
+    tile_of_block((M + C::BM - 1) / C::BM, nnt, mt, nt);
+    f(sm, mt * C::BM, nt);
+}
 
 template <class C, class O>
-__global__ void __launch_bounds__(C::THREADS)
+__global__ void __launch_bounds__(C::THREADS, 2)
 mxfp4_matmul_kernel(Mxfp4Pair x, int64_t M, int64_t N, int64_t nnt, O* __restrict__ out,
                     int64_t ld) {
-    with_row_tile<C>(M, nnt, [&](auto cfg, auto& sm, int64_t m0, int64_t nt) {
-        using T = decltype(cfg);
-        f32x16 acc[T::TM][T::TN];
-        gemm_tile<T>(x.a, M, x.K4, x.b, N, x.K4, x.K4, m0, nt * T::BN, sm, acc, x.scales);
-        store_tile<T, O>(acc, M, N, out, ld, sm, m0, nt * T::BN);
+    with_mxfp4_tile<C>(M, nnt, [&](auto& sm, int64_t m0, int64_t nt) {
+        f32x16 acc[C::TM][C::TN];
+        mxfp4_tile<C>(x, m0, nt * C::BN, sm, acc);
+        store_tile<C, O>(acc, M, N, out, ld, sm, m0, nt * C::BN);
     });
 }
 
 template <class C>
-__global__ void __launch_bounds__(C::THREADS)
+__global__ void __launch_bounds__(C::THREADS, 2)
 mxfp4_stats_kernel(Mxfp4Pair x, int64_t T, int64_t V, const int32_t* __restrict__ target,
                    float scale, int64_t nvt, float4* __restrict__ part, float* __restrict__ z_y) {
-    with_row_tile<C>(T, nvt, [&](auto cfg, auto& sm, int64_t m0, int64_t vt) {
-        using R = decltype(cfg);
-        stats_of_tile<R>(
-            [&](int64_t n0, f32x16(&acc)[R::TM][R::TN]) {
-                gemm_tile<R>(x.a, T, x.K4, x.b, V, x.K4, x.K4, m0, n0, sm, acc, x.scales);
-            },
-            T, V, target, scale, nvt, part, z_y, sm, m0, vt);
+    with_mxfp4_tile<C>(T, nvt, [&](auto& sm, int64_t m0, int64_t vt) {
+        stats_of_tile<C>(
+            [&](int64_t n0, f32x16(&acc)[C::TM][C::TN]) { mxfp4_tile<C>(x, m0, n0, sm, acc); }, T, V,
+            target, scale, nvt, part, z_y, sm, m0, vt);
     });
+}
+
+// out = A B^T for up to 32 rows of A (one row of panels): the workgroup takes 32 rows of B, its
+// waves panels w, w + 4, ... of both, kInFlight at a time all loaded before the first is
+// multiplied; the waves' sums are added in order through LDS. No LDS on the way in: a panel of
+// B is used once. FEWTIMES
+constexpr int kFewRows = 32, kFewWaves = 4, kInFlight = 4;
+template <class O>
+__global__ void __launch_bounds__(kFewWaves * 64)
+mxfp4_few_kernel(Mxfp4Pair x, int64_t M, int64_t N, O* __restrict__ out, int64_t ld) {
+    __shared__ f32x4 sums[kFewWaves][4][64];
+    const int tid = threadIdx.x, lane = tid & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int64_t n0 = (int64_t)blockIdx.x * kRun;
+    const u32x4* a = reinterpret_cast<const u32x4*>(x.a);
+    const u32x4* b = reinterpret_cast<const u32x4*>(x.b + (int64_t)blockIdx.x * x.slices * kPanel);
+    f32x16 acc = {};
+    for (int64_t s0 = wave; s0 < x.slices; s0 += kFewWaves * kInFlight) {
+        u32x4 bv[kInFlight][4], av[kInFlight][4];
+        uint32_t sb[kInFlight], sa[kInFlight];
+#pragma unroll
+        for (int p = 0; p < kInFlight; ++p) {
+            const int64_t s = s0 + p * kFewWaves;
+            if (s >= x.slices) break;
+            const u32x4* pb = b + s * (kPanel / 16);
+#pragma unroll
+            for (int ks = 0; ks < 4; ++ks) bv[p][ks] = __builtin_nontemporal_load(pb + ks * 64 + lane);
+            sb[p] = reinterpret_cast<const uint32_t*>(pb + kScalesAt / 16)[lane];
+        }
+#pragma unroll
+        for (int p = 0; p < kInFlight; ++p) {
+            const int64_t s = s0 + p * kFewWaves;
+            if (s >= x.slices) break;
+            const u32x4* pa = a + s * (kPanel / 16);
+#pragma unroll
+            for (int ks = 0; ks < 4; ++ks) av[p][ks] = pa[ks * 64 + lane];
+            sa[p] = reinterpret_cast<const uint32_t*>(pa + kScalesAt / 16)[lane];
+        }
+#pragma unroll
+        for (int p = 0; p < kInFlight; ++p) {
+            if (s0 + p * kFewWaves >= x.slices) break;
+#pragma unroll
+            for (int ks = 0; ks < 4; ++ks)
+                acc = mfma_mxfp4(ks, bv[p][ks], av[p][ks], acc, sb[p], sa[p]);
+        }
+    }
+#pragma unroll
+    for (int v = 0; v < 4; ++v)
+        sums[wave][v][lane] = f32x4{acc[4 * v], acc[4 * v + 1], acc[4 * v + 2], acc[4 * v + 3]};
+    __syncthreads();
+    // the wave's quarter of the columns: four adjacent ones of a row a lane
+    f32x4 t = sums[0][wave][lane];
+#pragma unroll
+    for (int w = 1; w < kFewWaves; ++w) t += sums[w][wave][lane];
+    const int64_t m = lane & 31, n = n0 + wave * 8 + (lane >> 5) * 4;
+    if (m >= M || n >= N) return;
+    O* dst = out + m * ld + n;
+    if constexpr (sizeof(O) == 2) {
+        const u32x2 pk = {pack_bf16x2(t[0], t[1]), pack_bf16x2(t[2], t[3])};
+        if (n + 4 <= N)
+            *reinterpret_cast<u32x2_at2*>(dst) = pk;
+        else
+            for (int e = 0; n + e < N; ++e) dst[e] = bf16_bits(t[e]);
+    } else {
+        if (n + 4 <= N)
+            *reinterpret_cast<u32x4_at4*>(dst) = __builtin_bit_cast(u32x4, t);
+        else
+            for (int e = 0; n + e < N; ++e) dst[e] = t[e];
+    }
 }
 
 bool bad_size(int64_t n) { return n < 1 || n > 0x7FFFFFFFll; }
 bool misaligned(const void* p, size_t to) { return reinterpret_cast<uintptr_t>(p) % to != 0; }
-bool bad_quantized(const void* packed, const void* scales, int64_t R, int64_t K) {
-    return !packed || !scales || bad_size(R) || bad_size(K) || misaligned(packed, 16) ||
-           misaligned(scales, 16);
+bool bad_quantized(const void* q, int64_t R, int64_t K) {
+    return !q || bad_size(R) || bad_size(K) || misaligned(q, 16);
 }
 size_t size_of(dart_dtype_t t) { return t == DART_BF16 ? 2 : 4; }
 bool bad_dtype(dart_dtype_t t) { return t != DART_BF16 && t != DART_F32; }
+// a run of panels is addressed by 32-bit byte offsets
+constexpr int64_t kMaxK = int64_t(1) << 24;
+static_assert((kMaxK / kSlice + 4) * kPanel < int64_t(1) << 31, "offsets of a run");
 
-Mxfp4Pair pair_of(const void* a, const void* as, int64_t M, const void* b, const void* bs,
-                  int64_t N, int64_t K) {
-    return {static_cast<const uint16_t*>(a), static_cast<const uint16_t*>(b),
-            {static_cast<const uint32_t*>(as), static_cast<const uint32_t*>(bs), runs_of(M),
-             runs_of(N)},
-            packed_ld(K)};
+Mxfp4Pair pair_of(const void* a, int64_t M, const void* b, int64_t N, int64_t K) {
+    return {static_cast<const uint8_t*>(a), static_cast<const uint8_t*>(b), runs_of(M), runs_of(N),
+            slices_of(K)};
+}
+
+int64_t column_tiles(int64_t N) { return (N + Mx256::BN - 1) / Mx256::BN; }
+
+// f(configuration) for M rows.
+template <class F>
+void with_mxfp4_cfg(int64_t M, F&& f) {
+    if (M <= 64)
+        f(Mx64{});
+    else if (M <= 128)
+        f(Mx128{});
+    else
+        f(Mx256{});
 }
 
 }  // namespace
 
 extern "C" {
 
-size_t dart_mxfp4_packed_bytes(int64_t R, int64_t K) {
+size_t dart_mxfp4_bytes(int64_t R, int64_t K) {
     if (bad_size(R) || bad_size(K)) return 0;
-    return (size_t)R * (size_t)slices_of(K) * 128;
-}
-
-size_t dart_mxfp4_scales_bytes(int64_t R, int64_t K) {
-    if (bad_size(R) || bad_size(K)) return 0;
-    return (size_t)runs_of(R) * (size_t)slices_of(K) * 256;
+    return (size_t)runs_of(R) * (size_t)slices_of(K) * kPanel;
 }
 
 dart_status_t dart_mxfp4_quantize(const void* x, dart_dtype_t dtype, int64_t R, int64_t K,
-                                  int64_t ld, void* packed, void* scales, hipStream_t stream) {
-    if (bad_dtype(dtype) || !x || ld < K || bad_quantized(packed, scales, R, K) ||
-        misaligned(x, size_of(dtype)))
+                                  int64_t ld, void* q, hipStream_t stream) {
+    if (bad_dtype(dtype) || !x || ld < K || bad_quantized(q, R, K) || misaligned(x, size_of(dtype)))
         return DART_ERR_INVALID_ARG;
     const int64_t blocks = runs_of(R) * slices_of(K);
     if (!grid_fits(blocks, kQuantThreads)) return DART_ERR_UNSUPPORTED;
     auto launch = [&](auto kernel, auto* p) {
         hipLaunchKernelGGL(kernel, dim3((unsigned)blocks), dim3(kQuantThreads), 0, stream, p, R, K,
-                           ld, slices_of(K), runs_of(R), static_cast<uint8_t*>(packed),
-                           static_cast<uint32_t*>(scales));
+                           ld, slices_of(K), static_cast<uint8_t*>(q));
     };
     if (dtype == DART_BF16)
         launch(mxfp4_quantize_kernel<uint16_t>, static_cast<const uint16_t*>(x));
@@ -334,18 +639,16 @@ dart_status_t dart_mxfp4_quantize(const void* x, dart_dtype_t dtype, int64_t R, 
     return hipGetLastError() == hipSuccess ? DART_OK : DART_ERR_HIP;
 }
 
-dart_status_t dart_mxfp4_dequantize(const void* packed, const void* scales, int64_t R, int64_t K,
-                                    dart_dtype_t dtype, void* out, int64_t ld_out,
-                                    hipStream_t stream) {
-    if (bad_dtype(dtype) || !out || ld_out < K || bad_quantized(packed, scales, R, K) ||
+dart_status_t dart_mxfp4_dequantize(const void* q, int64_t R, int64_t K, dart_dtype_t dtype,
+                                    void* out, int64_t ld_out, hipStream_t stream) {
+    if (bad_dtype(dtype) || !out || ld_out < K || bad_quantized(q, R, K) ||
         misaligned(out, size_of(dtype)))
         return DART_ERR_INVALID_ARG;
     const int64_t blocks = runs_of(R) * slices_of(K);
     if (!grid_fits(blocks, kQuantThreads)) return DART_ERR_UNSUPPORTED;
     auto launch = [&](auto kernel, auto* p) {
         hipLaunchKernelGGL(kernel, dim3((unsigned)blocks), dim3(kQuantThreads), 0, stream,
-                           static_cast<const uint8_t*>(packed), static_cast<const uint8_t*>(scales),
-                           R, K, slices_of(K), runs_of(R), p, ld_out);
+                           static_cast<const uint8_t*>(q), R, K, slices_of(K), p, ld_out);
     };
     if (dtype == DART_BF16)
         launch(mxfp4_dequantize_kernel<uint16_t>, static_cast<uint16_t*>(out));
@@ -354,52 +657,62 @@ dart_status_t dart_mxfp4_dequantize(const void* packed, const void* scales, int6
     return hipGetLastError() == hipSuccess ? DART_OK : DART_ERR_HIP;
 }
 
-dart_status_t dart_mxfp4_matmul(const void* a_packed, const void* a_scales, int64_t M,
-                                const void* b_packed, const void* b_scales, int64_t N, int64_t K,
+dart_status_t dart_mxfp4_matmul(const void* a, int64_t M, const void* b, int64_t N, int64_t K,
                                 dart_dtype_t dtype, void* out, int64_t ld_out, hipStream_t stream) {
-    if (bad_dtype(dtype) || !out || ld_out < N || bad_quantized(a_packed, a_scales, M, K) ||
-        bad_quantized(b_packed, b_scales, N, K) || misaligned(out, size_of(dtype)))
+    if (bad_dtype(dtype) || !out || ld_out < N || bad_quantized(a, M, K) ||
+        bad_quantized(b, N, K) || misaligned(out, size_of(dtype)))
         return DART_ERR_INVALID_ARG;
-    const int64_t nnt = vocab_tiles(N), nmt = (M + LmCfg::BM - 1) / LmCfg::BM;
-    if (!grid_fits(nmt * nnt, LmCfg::THREADS) || packed_ld(K) > kMaxLd) return DART_ERR_UNSUPPORTED;
-    const Mxfp4Pair x = pair_of(a_packed, a_scales, M, b_packed, b_scales, N, K);
-    with_tile<true>(tile_rows(M, N), M, N, [&](auto cfg) {
-        using C = decltype(cfg);
-        const dim3 grid((unsigned)((M + C::BM - 1) / C::BM * nnt)), block(C::THREADS);
-        if (dtype == DART_BF16)
-            hipLaunchKernelGGL((mxfp4_matmul_kernel<C, uint16_t>), grid, block, 0, stream, x, M, N,
-                               nnt, static_cast<uint16_t*>(out), ld_out);
+    const int64_t nnt = column_tiles(N);
+    if (!grid_fits((M + Mx256::BM - 1) / Mx256::BM * nnt, Mx256::THREADS) ||
+        !grid_fits(runs_of(N), kFewWaves * 64) || K > kMaxK)
+        return DART_ERR_UNSUPPORTED;
+    const Mxfp4Pair x = pair_of(a, M, b, N, K);
+    auto launch = [&](auto* p) {
+        using O = typename std::remove_pointer<decltype(p)>::type;
+        if (M <= kFewRows)
+            hipLaunchKernelGGL(mxfp4_few_kernel<O>, dim3((unsigned)runs_of(N)), dim3(kFewWaves * 64),
+                               0, stream, x, M, N, p, ld_out);
         else
-            hipLaunchKernelGGL((mxfp4_matmul_kernel<C, float>), grid, block, 0, stream, x, M, N,
-                               nnt, static_cast<float*>(out), ld_out);
-    });
+            with_mxfp4_cfg(M, [&](auto cfg) {
+                using C = decltype(cfg);
+                hipLaunchKernelGGL((mxfp4_matmul_kernel<C, O>),
+                                   dim3((unsigned)((M + C::BM - 1) / C::BM * nnt)),
+                                   dim3(C::THREADS), 0, stream, x, M, N, nnt, p, ld_out);
+            });
+    };
+    if (dtype == DART_BF16)
+        launch(static_cast<uint16_t*>(out));
+    else
+        launch(static_cast<float*>(out));
     return hipGetLastError() == hipSuccess ? DART_OK : DART_ERR_HIP;
 }
 
-dart_status_t dart_lmhead_mxfp4_tok_stats(const void* hidden_packed, const void* hidden_scales,
-                                          int64_t T, const void* weight_packed,
-                                          const void* weight_scales, int64_t V, int64_t d,
-                                          const int32_t* target, float inv_temp, float* logp,
-                                          float* entropy, float* lse, void* workspace,
-                                          size_t workspace_bytes, hipStream_t stream) {
-    if (bad_quantized(hidden_packed, hidden_scales, T, d) ||
-        bad_quantized(weight_packed, weight_scales, V, d))
-        return DART_ERR_INVALID_ARG;
+size_t dart_lmhead_mxfp4_stats_workspace_bytes(int64_t T, int64_t V) {
+    if (bad_size(T) || bad_size(V)) return 0;
+    return (size_t)T * (size_t)column_tiles(V) * sizeof(float4) + (size_t)T * sizeof(float);
+}
+
+dart_status_t dart_lmhead_mxfp4_tok_stats(const void* hidden, int64_t T, const void* weight,
+                                          int64_t V, int64_t d, const int32_t* target,
+                                          float inv_temp, float* logp, float* entropy, float* lse,
+                                          void* workspace, size_t workspace_bytes,
+                                          hipStream_t stream) {
+    if (bad_quantized(hidden, T, d) || bad_quantized(weight, V, d)) return DART_ERR_INVALID_ARG;
     if (!(inv_temp > 0.f) || isinf(inv_temp)) return DART_ERR_INVALID_ARG;
     if (!target || !logp || !entropy || !lse || !workspace || misaligned(workspace, 16) ||
-        workspace_bytes < dart_lmhead_stats_workspace_bytes(T, V))
+        workspace_bytes < dart_lmhead_mxfp4_stats_workspace_bytes(T, V))
         return DART_ERR_INVALID_ARG;
-    const int64_t nvt = vocab_tiles(V), nmt = (T + LmCfg::BM - 1) / LmCfg::BM;
-    if (!grid_fits(nmt * nvt, LmCfg::THREADS) ||
-        !grid_fits((T + kMergeWaves - 1) / kMergeWaves, kMergeWaves * 64) || packed_ld(d) > kMaxLd)
+    const int64_t nvt = column_tiles(V);
+    if (!grid_fits((T + Mx256::BM - 1) / Mx256::BM * nvt, Mx256::THREADS) ||
+        !grid_fits((T + kMergeWaves - 1) / kMergeWaves, kMergeWaves * 64) || d > kMaxK)
         return DART_ERR_UNSUPPORTED;
     if (const dart_status_t ck = dart_check::run(
             stream, {{dart_check::Item::Ids, target, T, V}}); ck != DART_OK)
         return ck;
-    const Mxfp4Pair x = pair_of(hidden_packed, hidden_scales, T, weight_packed, weight_scales, V, d);
+    const Mxfp4Pair x = pair_of(hidden, T, weight, V, d);
     float4* part = static_cast<float4*>(workspace);
     float* z_y = reinterpret_cast<float*>(part + T * nvt);
-    with_tile<true>(tile_rows(T, V), T, V, [&](auto cfg) {
+    with_mxfp4_cfg(T, [&](auto cfg) {
         using C = decltype(cfg);
         hipLaunchKernelGGL(mxfp4_stats_kernel<C>, dim3((unsigned)((T + C::BM - 1) / C::BM * nvt)),
                            dim3(C::THREADS), 0, stream, x, T, V, target, inv_temp, nvt, part, z_y);

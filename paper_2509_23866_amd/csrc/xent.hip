@@ -571,7 +571,7 @@ dart_status_t run_xent(const uint16_t* h, int64_t T, int64_t d, int64_t ld_h, co
     for (int64_t r0 = 0; r0 < T; r0 += P.rows) {
         const int64_t rows = T - r0 < P.rows ? T - r0 : P.rows;
         const uint16_t* hr = h_c + r0 * d;
-        with_tile<>(tile_rows(rows, V, d <= 1024 ? 57 : 54), rows, V, [&](auto cfg) {
+        with_tile(tile_rows(rows, V, d <= 1024 ? 57 : 54), rows, V, [&](auto cfg) {
             using C = decltype(cfg);
             const dim3 grid((unsigned)((rows + C::BM - 1) / C::BM * nvt));
             if (grads)

@@ -1,5 +1,5 @@
 """GPU tests of the four-bit operators against the float64 oracle: quantisation bit for bit
-(values, codes, scales and the buffers' padding), its inverse, the product and the token
+(values, codes, scales and the buffer's padding), its inverse, the product and the token
 statistics of a four-bit head.
 
 Tolerances. Quantised values are exact. A product's terms are exact in float32 (four-bit sizes
@@ -53,8 +53,7 @@ def _same(q, x):
 
     torch.cuda.synchronize()
     _, code, scale = mx.quantize(x)
-    assert np.array_equal(q.packed.cpu().numpy(), mx.packed_bytes(code))
-    assert np.array_equal(q.scales.cpu().numpy(), mx.scale_bytes(scale))
+    assert np.array_equal(q.data.cpu().numpy(), mx.buffer_bytes(code, scale))
 
 
 SHAPES = [(1, 1), (1, 31), (3, 32), (33, 33), (31, 255), (64, 256), (65, 257), (7, 1000), (200, 520),
@@ -159,10 +158,12 @@ def _product(rng, M, N, K):
     return a, b, va @ vb.T, np.abs(va) @ np.abs(vb).T
 
 
-# the tiles of 64, 128 and 256 rows and their edges, few rows, inner sizes inside a block and a slice
-PRODUCTS = [(1, 1, 1), (1, 300, 64), (2, 257, 255), (15, 33, 256), (16, 1000, 513), (17, 255, 1000),
+# few rows, the tiles of 64, 128 and 256 rows and their edges, inner sizes inside a block, a slice
+# and up to several rounds of the ring
+PRODUCTS = [(1, 1, 1), (1, 40, 4600), (32, 97, 1300), (3, 64, 2304), (1, 300, 64), (2, 257, 255), (15, 33, 256), (16, 1000, 513), (17, 255, 1000),
             (33, 256, 320), (64, 1025, 776), (65, 129, 2048), (128, 511, 264), (129, 700, 96),
-            (257, 130, 512), (300, 2050, 40), (700, 300, 1024)]
+            (257, 130, 512), (300, 2050, 40), (700, 300, 1024),
+            (40, 260, 1536), (100, 130, 1793), (300, 129, 1281), (257, 500, 4600), (65, 300, 3600)]
 
 
 @pytest.mark.parametrize("out", ["bf16", "f32"])
@@ -203,7 +204,7 @@ def test_matmul_into_a_wider_matrix(M, N, out):
         assert bool((big == 7.0).all())
 
 
-STATS = [(1, 8, 1), (1, 300, 1000), (3, 40, 5), (16, 256, 700), (64, 512, 4099), (129, 200, 513),
+STATS = [(1, 8, 1), (64, 1100, 130), (130, 2100, 400), (1, 300, 1000), (3, 40, 5), (16, 256, 700), (64, 512, 4099), (129, 200, 513),
          (257, 776, 1300), (600, 128, 2000)]
 
 
@@ -351,7 +352,7 @@ def test_refusals_with_tensors():
     with pytest.raises(ValueError):
         dart.dart_mxfp4_dequantize(q._replace(rows=80))
     with pytest.raises(ValueError):
-        dart.dart_mxfp4_dequantize(q._replace(scales=q.scales[1:]))
+        dart.dart_mxfp4_dequantize(q._replace(data=q.data[1:]))
     with pytest.raises(ValueError):
         dart.dart_mxfp4_matmul(x[:, :32].contiguous(), q)
     with pytest.raises(TypeError):

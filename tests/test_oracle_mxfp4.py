@@ -1,5 +1,5 @@
 """Pins of the MXFP4 oracle: the format's numbers, its rounding by brute force, its scale's
-closed forms, and the buffers' places counted one by one."""
+closed forms, and the buffer's places counted one by one."""
 
 import math
 
@@ -55,21 +55,22 @@ def test_values_are_near_and_idempotent():
     assert s[2, 1] == 255 and s[3, 3] == 255
 
 
-def test_buffers_place_by_place():
+def test_buffer_place_by_place():
     R, K = 35, 300
     rng = np.random.default_rng(1)
-    code = rng.integers(0, 16, (R, K)).astype(np.uint8)
+    code = rng.integers(1, 16, (R, K)).astype(np.uint8)
     scale = rng.integers(1, 255, (R, 10)).astype(np.uint8)
-    p, s = mx.packed_bytes(code), mx.scale_bytes(scale)
-    assert p.shape == (R, 256) and s.size == 2 * 2 * 256
+    q = mx.buffer_bytes(code, scale)
+    assert q.size == 2 * 2 * 4352
+    left = q.copy()
     for r in range(R):
-        for k in range(512):
-            nib = p[r, k // 2] >> (4 * (k % 2)) & 15
-            assert nib == (code[r, k] if k < K else 0)
-    left = s.copy()
-    for r in range(R):
+        for k in range(K):
+            b, j = k % 256 // 32, k % 32
+            at = (r // 32 * 2 + k // 256) * 4352 + b % 4 * 1024 + (b // 4 * 32 + r % 32) * 16 + j // 2
+            assert q[at] >> (4 * (j % 2)) & 15 == code[r, k]
+            left[at] &= 0xF0 if j % 2 == 0 else 0x0F
         for b in range(10):
-            at = (((b // 8) * 2 + r // 32) * 64 + (b % 8) // 4 * 32 + r % 32) * 4 + b % 4
-            assert s[at] == scale[r, b]
+            at = (r // 32 * 2 + b // 8) * 4352 + 4096 + (b % 8 // 4 * 32 + r % 32) * 4 + b % 4
+            assert q[at] == scale[r, b]
             left[at] = 0
     assert not left.any()
