@@ -1025,6 +1025,11 @@ def dart_lmhead_xent_fwd(hidden, weight, target, label_smoothing=0.0, z_loss=0.0
     (1 - eps) (lse - z_y) + eps (lse - mean z) + z_loss lse^2; ``reduction``: "mean" over the rows
     that count, or "sum". ``workspace``: "auto" (allocated here) or a uint8 device tensor of
     dart_lmhead_xent_fwd_workspace_bytes(T, d, V) bytes."""
+    if stream is None and isinstance(workspace, str) and workspace == "auto":
+        out = _nat().lmhead_xent_fwd(hidden, weight, target, label_smoothing, z_loss,
+                                     DART_XENT.get(reduction))
+        if out is not None:
+            return _made(out, "dart_lmhead_xent_fwd")
     torch = _torch()
     dev, T, d, V, config = _xent_inputs(hidden, weight, target, label_smoothing, z_loss, reduction)
     loss = torch.empty(1, dtype=torch.float32, device=dev)
@@ -1045,11 +1050,19 @@ def dart_lmhead_xent_fwd_bwd(hidden, weight, target, label_smoothing=0.0, z_loss
     time are kept in the workspace (default: lmhead_xent_plan's). ``want`` says which gradients to
     form (None is returned for the other). ``workspace``: "auto" (allocated here) or a uint8 device
     tensor of dart_lmhead_xent_workspace_bytes(T, d, V, chunk_rows) bytes."""
-    torch = _torch()
-    dev, T, d, V, config = _xent_inputs(hidden, weight, target, label_smoothing, z_loss, reduction)
-    want_h, want_w = want
+    want_h, want_w = map(bool, want)
     if not (want_h or want_w):
         raise ValueError("want at least one gradient")
+    if (stream is None and dhidden is None and dweight is None and isinstance(workspace, str)
+            and workspace == "auto" and getattr(hidden, "ndim", 0) == getattr(weight, "ndim", 0) == 2):
+        T, V = hidden.shape[0], weight.shape[0]
+        rows = lmhead_xent_plan(T, V) if chunk_rows is None else max(1, min(int(chunk_rows), T))
+        out = _nat().lmhead_xent_fwd_bwd(hidden, weight, target, label_smoothing, z_loss,
+                                         DART_XENT.get(reduction), rows, want_h, want_w)
+        if out is not None:
+            return _made(out, "dart_lmhead_xent_fwd_bwd")
+    torch = _torch()
+    dev, T, d, V, config = _xent_inputs(hidden, weight, target, label_smoothing, z_loss, reduction)
     bf16 = torch.bfloat16
     chunk_rows = lmhead_xent_plan(T, V) if chunk_rows is None else max(1, min(int(chunk_rows), T))
     dhidden = _out_matrix("dhidden", dhidden, (T, d), bf16, dev) if want_h else None
@@ -1123,6 +1136,10 @@ def dart_mxfp4_quantize(x, out=None, stream=None):
     values share the scale 2^max(floor(log2 of the largest size) - 2, -127), and each becomes the
     nearest of 0, 0.5, 1, 1.5, 2, 3, 4, 6 times it (ties to the even code, larger ones 6). A block
     with an infinity or a NaN stands for NaN. ``out``: an Mxfp4 of the same shape to write to."""
+    if out is None and stream is None:
+        made = _nat().mxfp4_quantize(x)
+        if made is not None:
+            return Mxfp4(_made(made, "dart_mxfp4_quantize")[0], *x.shape)
     torch = _torch()
     if not isinstance(x, torch.Tensor) or str(x.dtype) not in _FLOATS:
         raise TypeError("x must be a float32 or bfloat16 tensor")
@@ -1145,6 +1162,10 @@ def dart_mxfp4_quantize(x, out=None, stream=None):
 
 def dart_mxfp4_dequantize(q, dtype=None, out=None, stream=None):
     """The values that an Mxfp4 stands for, as a [rows, cols] bfloat16 (default) or float32 tensor."""
+    if out is None and stream is None:
+        made = _nat().mxfp4_dequantize(q, dtype)
+        if made is not None:
+            return _made(made, "dart_mxfp4_dequantize")[0]
     torch = _torch()
     _check_mxfp4("q", q)
     dtype = (torch.bfloat16 if out is None else out.dtype) if dtype is None else dtype
@@ -1170,6 +1191,10 @@ def dart_mxfp4_matmul(a, b, dtype=None, out=None, stream=None):
     """a @ b^T of Mxfp4 matrices a [M, K] and b [N, K], summed in float32, as a [M, N] bfloat16
     (default) or float32 tensor: the logits of tokens ``a`` under a head ``b`` kept in four bits.
     ``a`` may be a float32 or bfloat16 tensor, which is quantised first."""
+    if out is None and stream is None:
+        made = _nat().mxfp4_matmul(a, b, dtype)
+        if made is not None:
+            return _made(made, "dart_mxfp4_matmul", "dart_mxfp4_quantize")[0]
     torch = _torch()
     _check_mxfp4("b", b)
     dtype = (torch.bfloat16 if out is None else out.dtype) if dtype is None else dtype
@@ -1193,6 +1218,11 @@ def dart_lmhead_mxfp4_tok_stats(hidden, weight, target, inv_temp=1.0, logp=None,
     log-probs of a rollout policy whose head is kept in four bits, without materialising the logits.
     ``workspace``: "auto" (allocated here) or a uint8 device tensor of
     dart_lmhead_mxfp4_stats_workspace_bytes(T, V) bytes."""
+    if (logp is None and entropy is None and lse is None and stream is None
+            and isinstance(workspace, str) and workspace == "auto"):
+        out = _nat().lmhead_mxfp4_tok_stats(hidden, weight, target, inv_temp)
+        if out is not None:
+            return _made(out, "dart_lmhead_mxfp4_tok_stats", "dart_mxfp4_quantize")
     torch = _torch()
     _check_mxfp4("weight", weight)
     dev = weight.data.device

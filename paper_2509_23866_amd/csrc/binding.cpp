@@ -12,8 +12,10 @@
 // 512 x 4096 and 34 us at 96 x 152064.
 #include <Python.h>
 #include <ATen/ATen.h>
+#include <c10/hip/HIPFunctions.h>
 #include <c10/hip/HIPStream.h>
 #include <dlfcn.h>
+#include <torch/csrc/Dtype.h>
 #include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/python_variable.h>
 
@@ -26,7 +28,12 @@ namespace {
     F(dart_tis_grad) F(dart_tis_grad_ex) F(dart_grpo_advantage)                  \
     F(dart_step_select_groups) F(dart_tis_loss_fwd_ex)                           \
     F(dart_lmhead_tok_stats) F(dart_lmhead_tok_stats_ex)                         \
-    F(dart_tis_loss_split_workspace_bytes) F(dart_lmhead_stats_workspace_bytes)
+    F(dart_tis_loss_split_workspace_bytes) F(dart_lmhead_stats_workspace_bytes)  \
+    F(dart_lmhead_xent_fwd) F(dart_lmhead_xent_fwd_workspace_bytes)              \
+    F(dart_lmhead_xent_fwd_bwd) F(dart_lmhead_xent_workspace_bytes)              \
+    F(dart_mxfp4_bytes) F(dart_mxfp4_quantize) F(dart_mxfp4_dequantize)          \
+    F(dart_mxfp4_matmul) F(dart_lmhead_mxfp4_tok_stats)                          \
+    F(dart_lmhead_mxfp4_stats_workspace_bytes)
 
 struct Lib {
 #define DECLARE(name) decltype(&::name) name = nullptr;
@@ -419,6 +426,196 @@ NATIVE(lmhead_tok_stats, 4)
     return st == DART_OK ? tuple(o.logp, o.entropy, o.lse) : failed(0, st);
 NATIVE_END
 
+// The null stream is the current device's: tensors of another are left to the Python path.
+bool current(at::Device dev) { return c10::hip::current_device() == dev.index(); }
+
+int64_t row_stride(const Tensor& t) { return t.size(0) > 1 ? t.stride(0) : t.size(1); }
+
+struct Xent {
+    const Tensor *h = nullptr, *w = nullptr;
+    const int32_t* y = nullptr;
+    int64_t T, V, d;
+    at::Device dev{at::kCPU};
+    dart_xent_config_t config;
+    Tensor loss, tok, n, ws;
+    size_t bytes = 0;
+
+    // hidden, weight, target, label_smoothing, z_loss, reduction (its number)
+    bool take(PyObject* const* a) {
+        double eps, lam, reduction;
+        if (!matrix(a[0], h) || !matrix(a[1], w) || w->device() != h->device() ||
+            w->size(1) != h->size(1) || !vec(a[2], at::kInt, h->size(0), h->device(), y) ||
+            !number(a[3], eps) || !number(a[4], lam) || !number(a[5], reduction) ||
+            !current(h->device()))
+            return false;
+        T = h->size(0), V = w->size(0), d = h->size(1), dev = h->device();
+        config = {(float)eps, (float)lam, (int32_t)reduction};
+        return true;
+    }
+    void make(size_t bytes_) {
+        bytes = bytes_;
+        loss = empty({1}, at::kFloat, dev), tok = empty({T}, at::kFloat, dev);
+        n = empty({1}, at::kInt, dev), ws = empty({(int64_t)bytes}, at::kByte, dev);
+    }
+};
+
+NATIVE(lmhead_xent_fwd, 6)
+    Xent x;
+    if (!x.take(a)) Py_RETURN_NONE;
+    x.make(lib.dart_lmhead_xent_fwd_workspace_bytes(x.T, x.d, x.V));
+    const hipStream_t s = stream_of(x.dev);
+    const dart_status_t st = call([&] {
+        return lib.dart_lmhead_xent_fwd(x.h->data_ptr(), x.T, x.d, row_stride(*x.h),
+                                        x.w->data_ptr(), x.V, row_stride(*x.w), x.y, &x.config,
+                                        f32(x.loss), f32(x.tok), i32(x.n), x.ws.data_ptr(), x.bytes,
+                                        s);
+    });
+    return st == DART_OK ? tuple(x.loss, x.tok, x.n) : failed(0, st);
+NATIVE_END
+
+// those of lmhead_xent_fwd, chunk_rows, whether dhidden and dweight are wanted
+NATIVE(lmhead_xent_fwd_bwd, 9)
+    Xent x;
+    double chunk;
+    if (!x.take(a) || !number(a[6], chunk)) Py_RETURN_NONE;
+    const int64_t rows = (int64_t)chunk;
+    Tensor dh, dw;
+    if (a[7] == Py_True) dh = empty({x.T, x.d}, at::kBFloat16, x.dev);
+    if (a[8] == Py_True) dw = empty({x.V, x.d}, at::kBFloat16, x.dev);
+    x.make(lib.dart_lmhead_xent_workspace_bytes(x.T, x.d, x.V, rows));
+    const hipStream_t s = stream_of(x.dev);
+    const dart_status_t st = call([&] {
+        return lib.dart_lmhead_xent_fwd_bwd(
+            x.h->data_ptr(), x.T, x.d, row_stride(*x.h), x.w->data_ptr(), x.V, row_stride(*x.w),
+            x.y, &x.config, f32(x.loss), f32(x.tok), i32(x.n), dh.defined() ? dh.data_ptr() : nullptr,
+            x.d, dw.defined() ? dw.data_ptr() : nullptr, x.d, rows, x.ws.data_ptr(), x.bytes, s);
+    });
+    return st == DART_OK ? tuple(x.loss, x.tok, x.n, dh, dw) : failed(0, st);
+NATIVE_END
+
+// A quantised matrix: the binding's (data, rows, cols), or what quantising a tensor gives.
+struct Quantized {
+    Tensor data;
+    int64_t rows = 0, cols = 0;
+    const Tensor* raw = nullptr;  // not yet quantised
+
+    bool take_mxfp4(PyObject* o) {
+        if (!PyTuple_Check(o) || PyTuple_CheckExact(o) || PyTuple_GET_SIZE(o) != 3) return false;
+        const Tensor* t = plain(PyTuple_GET_ITEM(o, 0));
+        double r, c;
+        if (!t || !number(PyTuple_GET_ITEM(o, 1), r) || !number(PyTuple_GET_ITEM(o, 2), c))
+            return false;
+        rows = (int64_t)r, cols = (int64_t)c;
+        const size_t n = lib.dart_mxfp4_bytes(rows, cols);
+        if (n == 0 || t->scalar_type() != at::kByte || !t->is_contiguous() ||
+            (size_t)t->numel() != n || reinterpret_cast<uintptr_t>(t->data_ptr()) % 16)
+            return false;
+        data = *t;
+        return true;
+    }
+    bool take_raw(PyObject* o) {
+        raw = plain(o);
+        if (!raw || raw->dim() != 2 || raw->numel() == 0 ||
+            (raw->size(1) > 1 && raw->stride(1) != 1) || row_stride(*raw) < raw->size(1) ||
+            (raw->scalar_type() != at::kFloat && raw->scalar_type() != at::kBFloat16))
+            return false;
+        rows = raw->size(0), cols = raw->size(1);
+        return true;
+    }
+    at::Device device() const { return raw ? raw->device() : data.device(); }
+    void make() {
+        if (raw) data = empty({(int64_t)lib.dart_mxfp4_bytes(rows, cols)}, at::kByte, raw->device());
+    }
+    // the call that quantises, where there is one to make
+    dart_status_t quantize(hipStream_t s) const {
+        if (!raw) return DART_OK;
+        return lib.dart_mxfp4_quantize(raw->data_ptr(),
+                                       raw->scalar_type() == at::kFloat ? DART_F32 : DART_BF16, rows,
+                                       cols, row_stride(*raw), data.data_ptr(), s);
+    }
+};
+
+// bfloat16 for None; false for what is neither it nor float32
+bool float_type(PyObject* o, at::ScalarType& t) {
+    t = at::kBFloat16;
+    if (o == Py_None) return true;
+    if (!THPDtype_Check(o)) return false;
+    t = reinterpret_cast<THPDtype*>(o)->scalar_type;
+    return t == at::kBFloat16 || t == at::kFloat;
+}
+dart_dtype_t dtype_of(at::ScalarType t) { return t == at::kFloat ? DART_F32 : DART_BF16; }
+
+// x: the quantised matrix's bytes
+NATIVE(mxfp4_quantize, 1)
+    Quantized q;
+    if (!q.take_raw(a[0]) || !current(q.device())) Py_RETURN_NONE;
+    q.make();
+    const hipStream_t s = stream_of(q.device());
+    const dart_status_t st = call([&] { return q.quantize(s); });
+    return st == DART_OK ? tuple(q.data) : failed(0, st);
+NATIVE_END
+
+// q, dtype
+NATIVE(mxfp4_dequantize, 2)
+    Quantized q;
+    at::ScalarType t;
+    if (!q.take_mxfp4(a[0]) || !float_type(a[1], t) || !current(q.device())) Py_RETURN_NONE;
+    const Tensor out = empty({q.rows, q.cols}, t, q.device());
+    const hipStream_t s = stream_of(q.device());
+    const dart_status_t st = call([&] {
+        return lib.dart_mxfp4_dequantize(q.data.data_ptr(), q.rows, q.cols, dtype_of(t),
+                                         out.data_ptr(), q.cols, s);
+    });
+    return st == DART_OK ? tuple(out) : failed(0, st);
+NATIVE_END
+
+// a (an Mxfp4 or a tensor), b, dtype
+NATIVE(mxfp4_matmul, 3)
+    Quantized x, w;
+    at::ScalarType t;
+    if (!w.take_mxfp4(a[1]) || !float_type(a[2], t) || !(x.take_mxfp4(a[0]) || x.take_raw(a[0])) ||
+        x.cols != w.cols || x.device() != w.device() || !current(w.device()))
+        Py_RETURN_NONE;
+    x.make();
+    const Tensor out = empty({x.rows, w.rows}, t, w.device());
+    const hipStream_t s = stream_of(w.device());
+    int place = 1;
+    const dart_status_t st = call([&] {
+        const dart_status_t q = x.quantize(s);
+        if (q != DART_OK) return q;
+        place = 0;
+        return lib.dart_mxfp4_matmul(x.data.data_ptr(), x.rows, w.data.data_ptr(), w.rows, w.cols,
+                                     dtype_of(t), out.data_ptr(), w.rows, s);
+    });
+    return st == DART_OK ? tuple(out) : failed(place, st);
+NATIVE_END
+
+// hidden (an Mxfp4 or a tensor), weight, target, inv_temp
+NATIVE(lmhead_mxfp4_tok_stats, 4)
+    Quantized h, w;
+    const int32_t* y;
+    double it;
+    if (!w.take_mxfp4(a[1]) || !(h.take_mxfp4(a[0]) || h.take_raw(a[0])) || h.cols != w.cols ||
+        h.device() != w.device() || !vec(a[2], at::kInt, h.rows, w.device(), y) ||
+        !number(a[3], it) || !current(w.device()))
+        Py_RETURN_NONE;
+    h.make();
+    const TokStats o(h.rows, w.device());
+    const size_t bytes = lib.dart_lmhead_mxfp4_stats_workspace_bytes(h.rows, w.rows);
+    const Tensor ws = empty({(int64_t)bytes}, at::kByte, w.device());
+    const hipStream_t s = stream_of(w.device());
+    int place = 1;
+    const dart_status_t st = call([&] {
+        const dart_status_t q = h.quantize(s);
+        if (q != DART_OK) return q;
+        place = 0;
+        return lib.dart_lmhead_mxfp4_tok_stats(h.data.data_ptr(), h.rows, w.data.data_ptr(), w.rows,
+                                               w.cols, y, (float)it, f32(o.logp), f32(o.entropy),
+                                               f32(o.lse), ws.data_ptr(), bytes, s);
+    });
+    return st == DART_OK ? tuple(o.logp, o.entropy, o.lse) : failed(place, st);
+NATIVE_END
+
 // open(path): the C functions of the library at path.
 PyObject* open_lib(PyObject*, PyObject* arg) {
     const char* path = PyUnicode_AsUTF8(arg);
@@ -439,7 +636,9 @@ PyObject* open_lib(PyObject*, PyObject* arg) {
 PyMethodDef methods[] = {
     ENTRY(tok_stats), ENTRY(select_tis_loss_fwd), ENTRY(tis_grad), ENTRY(policy_update),
     ENTRY(grpo_advantage), ENTRY(step_select_groups), ENTRY(tis_loss_fwd_ex),
-    ENTRY(lmhead_tok_stats), {"open", open_lib, METH_O, nullptr}, {nullptr, nullptr, 0, nullptr}};
+    ENTRY(lmhead_tok_stats), ENTRY(lmhead_xent_fwd), ENTRY(lmhead_xent_fwd_bwd),
+    ENTRY(mxfp4_quantize), ENTRY(mxfp4_dequantize), ENTRY(mxfp4_matmul),
+    ENTRY(lmhead_mxfp4_tok_stats), {"open", open_lib, METH_O, nullptr}, {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module_def = {PyModuleDef_HEAD_INIT, "_native", nullptr, -1, methods,
                           nullptr, nullptr, nullptr, nullptr};
 
