@@ -104,24 +104,6 @@ __attribute__((visibility("hidden"))) dart_status_t launch_bwd_gemms(
     int64_t part_stride, const Grad& dw_out, bool dw_acc, hipStream_t stream, const int32_t* dh_map,
     const int32_t* dyn_rows, int64_t dyn_base, const float* scale);
 
-// Parts of a block's dh sum. dh has rows / 256 x d / 256 tiles, each a sum over
-// the block's whole vocabulary, and one launch holds them and dW's tiles, the
-// same work in many short sums: while dh's tiles fill less than half of the
-// compute units the launch waits for them (at 1000 rows, d = 3584, V = 152064:
-// 56 tiles of 2376 slices, 3.62 ms; in 2, 4 or 9 parts 2.10, 1.95 or 2.02 ms, adding
-// them up 7, 17 or 37 us more). So that at least half
-// and at most all of the units have a part, none shorter than least slices of 64.
-__attribute__((visibility("hidden"))) int64_t dh_parts(int64_t rows, int64_t d, int64_t cols,
-                                                       int64_t least);
-
-// The ksplit parts of dh (each [rows, d] fp32, part_stride elements apart) added up in
-// part order into out: row r to row r, or (map, its first entry that of row 0) to row
-// map[r]; with dyn_rows rows below *dyn_rows - dyn_base.
-__attribute__((visibility("hidden"))) void launch_sum_parts(
-    const float* parts, int64_t ksplit, int64_t part_stride, int64_t rows, int64_t d,
-    const int32_t* map, const Grad& out, const int32_t* dyn_rows, int64_t dyn_base,
-    hipStream_t stream);
-
 // dst [rows, cols] in bf16 from fp32 rows of cols elements.
 __attribute__((visibility("hidden"))) void launch_to_bf16(const float* src, int64_t rows,
                                                           int64_t cols, const Grad& dst,

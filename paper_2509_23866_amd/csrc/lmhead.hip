@@ -839,9 +839,6 @@ constexpr uint32_t kBackwardFlags = DART_LMHEAD_SKIP_ZERO_ROWS | DART_LMHEAD_BF1
 int64_t ceil8(int64_t x) { return (x + 7) / 8 * 8; }
 size_t align256(size_t x) { return (x + 255) / 256 * 256; }
 
-// slices of 64 vocabulary entries in the shortest part of dh's sum
-constexpr int64_t kMinPartSlices = 32;
-
 // How a backward call runs and where its parts sit in the workspace (byte
 // offsets, each part 256-byte aligned; total is the end of the last part).
 struct BackwardPlan {
@@ -871,6 +868,22 @@ struct BackwardPlan {
 bool leaves_zero_rows_out(int64_t T, int64_t d, int64_t V) {
     return T >= 256 && (double)T * (double)V * (double)d >= 1e11 &&
            (double)T * (double)(6 * d + 20) <= double(128 << 20);
+}
+
+// Parts of a block's dh sum. dh has rows / 256 x d / 256 tiles, each a sum over
+// the block's whole vocabulary, and one launch holds them and dW's tiles, the
+// same work in many short sums: while dh's tiles fill less than half of the
+// compute units the launch waits for them (at 1000 rows, d = 3584, V = 152064:
+// 56 tiles of 2376 slices, 3.62 ms; in 2, 4 or 9 parts 2.10, 1.95 or 2.02 ms, adding
+// them up 7, 17 or 37 us more). So that at least half
+// and at most all of the units have a part, none shorter than kMinPartSlices.
+constexpr int64_t kMinPartSlices = 32;
+int64_t dh_parts(int64_t rows, int64_t d, int64_t cols) {
+    const int64_t tiles =
+        ((rows + LmCfg::BM - 1) / LmCfg::BM) * ((d + LmCfg::BN - 1) / LmCfg::BN);
+    const int64_t by_units = kUnits / tiles, by_k = cols / (LmCfg::BK * kMinPartSlices);
+    const int64_t n = by_units < by_k ? by_units : by_k;
+    return n > 1 ? n : 1;
 }
 
 // total = 0 when the sizes do not fit the address arithmetic.
@@ -909,7 +922,7 @@ BackwardPlan plan_backward(int64_t T, int64_t d, int64_t V, int64_t chunk_rows,
     };
     if (P.skip) take_rows();
     P.total = end;
-    P.ksplit = lmhead::dh_parts(P.rows, d, P.cols, kMinPartSlices);
+    P.ksplit = dh_parts(P.rows, d, P.cols);
     P.compact = !P.skip && leaves_zero_rows_out(T, d, V);
     if (P.compact) take_rows();
     if (P.ksplit > 1) P.parts = take((size_t)P.ksplit * (size_t)P.rows * (size_t)d * 4);
@@ -996,29 +1009,6 @@ void lmhead::launch_to_bf16(const float* src, int64_t rows, int64_t cols, const 
                        static_cast<uint16_t*>(dst.p), dst.ld);
 }
 
-void lmhead::launch_sum_parts(const float* parts, int64_t ksplit, int64_t part_stride, int64_t rows,
-                              int64_t d, const int32_t* map, const Grad& out,
-                              const int32_t* dyn_rows, int64_t dyn_base, hipStream_t stream) {
-    const int64_t blocks = (rows * d / 4 + 255) / 256;
-    const dim3 grid((unsigned)(blocks < kRowBlocks ? blocks : kRowBlocks));
-    if (out.bf16)
-        hipLaunchKernelGGL(sum_parts_kernel<uint16_t>, grid, dim3(256), 0, stream, parts, ksplit,
-                           part_stride, rows, d, map, static_cast<uint16_t*>(out.p), out.ld,
-                           dyn_rows, dyn_base);
-    else
-        hipLaunchKernelGGL(sum_parts_kernel<float>, grid, dim3(256), 0, stream, parts, ksplit,
-                           part_stride, rows, d, map, static_cast<float*>(out.p), out.ld, dyn_rows,
-                           dyn_base);
-}
-
-int64_t lmhead::dh_parts(int64_t rows, int64_t d, int64_t cols, int64_t least) {
-    const int64_t tiles =
-        ((rows + LmCfg::BM - 1) / LmCfg::BM) * ((d + LmCfg::BN - 1) / LmCfg::BN);
-    const int64_t by_units = kUnits / tiles, by_k = cols / (LmCfg::BK * least);
-    const int64_t n = by_units < by_k ? by_units : by_k;
-    return n > 1 ? n : 1;
-}
-
 namespace {
 
 // The gradient pass over rows [0, T) of h in blocks of rows x vocabulary
@@ -1052,8 +1042,16 @@ dart_status_t backward_core(const uint16_t* h, int64_t T, int64_t d,
     const bool via_h = !parts && dh.bf16 && C < V, via_w = dw.bf16 && R < T;
     const bool put = map && !parts && !via_h;
     auto sum_parts = [&](const float* p, int64_t n, int64_t stride, int64_t r0, int64_t rows) {
-        lmhead::launch_sum_parts(p, n, stride, rows, d, map ? map + r0 : nullptr,
-                                 map ? dh : Grad{dh.row(r0), dh.ld, dh.bf16}, dyn_rows, r0, stream);
+        const int64_t blocks = (rows * d / 4 + 255) / 256;
+        const dim3 grid((unsigned)(blocks < kRowBlocks ? blocks : kRowBlocks));
+        const int32_t* m = map ? map + r0 : nullptr;
+        void* out = map ? dh.p : dh.row(r0);
+        if (dh.bf16)
+            hipLaunchKernelGGL(sum_parts_kernel<uint16_t>, grid, dim3(256), 0, stream, p, n, stride,
+                               rows, d, m, static_cast<uint16_t*>(out), dh.ld, dyn_rows, r0);
+        else
+            hipLaunchKernelGGL(sum_parts_kernel<float>, grid, dim3(256), 0, stream, p, n, stride,
+                               rows, d, m, static_cast<float*>(out), dh.ld, dyn_rows, r0);
     };
     const Grad sum_h = via_h ? Grad{acc_h, d, false} : dh;
     const Grad sum_w = via_w ? Grad{acc_w, d, false} : dw;

@@ -412,22 +412,48 @@ xent_gather_kernel(const int32_t* __restrict__ map, const int32_t* __restrict__ 
     }
 }
 
-// One workgroup: the loss, summed in fp64 in a fixed order.
-constexpr int kLossThreads = 1024;
-__global__ void __launch_bounds__(kLossThreads)
-xent_loss_kernel(const float* __restrict__ tok_loss, int64_t T, int mean,
-                 const int32_t* __restrict__ count, float* __restrict__ loss) {
-    __shared__ double waves[kLossThreads / 64];
+// The last launch. Workgroup 0 (where loss is not null): the loss, summed in fp64 in a fixed
+// order. The others (where parts is not null): the ksplit parts of the block's rows of dh
+// ([rows, d] fp32 each, stride elements apart) added up in part order, rounded to bf16 and put
+// where they belong (row map[r]), rows below *n_rows - base; four columns a work-item at a time,
+// grid-stride.
+constexpr int kFinishThreads = 512;
+struct DhParts {
+    const float* parts;
+    int64_t ksplit, stride, rows, d;
+    const int32_t* map;
+    uint16_t* dh;
+    int64_t ld_dh, base;
+};
+__global__ void __launch_bounds__(kFinishThreads)
+xent_finish_kernel(const float* __restrict__ tok_loss, int64_t T, int mean,
+                   const int32_t* __restrict__ n_rows, float* __restrict__ loss, DhParts p) {
     const int tid = threadIdx.x;
+    const int64_t n = *n_rows;
+    if (blockIdx.x > 0 || !loss) {
+        const int64_t live = n - p.base, rows = live < p.rows ? live : p.rows;
+        const int64_t first = blockIdx.x - (loss ? 1 : 0), wgs = gridDim.x - (loss ? 1 : 0);
+        for (int64_t i = first * kFinishThreads + tid; i * 4 < rows * p.d; i += wgs * kFinishThreads) {
+            const f32x4* q = reinterpret_cast<const f32x4*>(p.parts) + i;  // d % 8 == 0
+            f32x4 x = q[0];
+#pragma unroll 8
+            for (int64_t k = 1; k < p.ksplit; ++k) x += q[k * (p.stride / 4)];
+            const int64_t r = i * 4 / p.d;
+            uint16_t* o = p.dh + p.map[r] * p.ld_dh + (i * 4 - r * p.d);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) o[e] = bf16_bits(x[e]);
+        }
+        return;
+    }
+    __shared__ double waves[kFinishThreads / 64];
     double x = 0.0;
-    for (int64_t t = tid; t < T; t += kLossThreads) x += (double)tok_loss[t];
+    for (int64_t t = tid; t < T; t += kFinishThreads) x += (double)tok_loss[t];
 #pragma unroll
     for (int off = 32; off >= 1; off >>= 1) x += __shfl_xor(x, off);
     if ((tid & 63) == 0) waves[tid >> 6] = x;
     __syncthreads();
     if (tid) return;
-    for (int k = 1; k < kLossThreads / 64; ++k) x += waves[k];
-    const int n = count[0];
+    for (int k = 1; k < kFinishThreads / 64; ++k) x += waves[k];
     loss[0] = (float)(mean && n > 0 ? x / (double)n : x);
 }
 
@@ -463,10 +489,22 @@ grad_scale_kernel(X* __restrict__ x, int64_t rows, int64_t cols, int64_t ld,
 constexpr int64_t kRowBlocksMost = 65536;
 int64_t ceil8(int64_t x) { return (x + 7) / 8 * 8; }
 
-// Slices of 64 vocabulary entries in the shortest part of dh's sum: a slice takes 1 us where few
-// tiles run, adding the parts up 4 us (48 rows of V = 4000, d = 512: the products 66 us in one
-// part of 63 slices, PARTSUS us in 7).
-constexpr int64_t kMinPartSlices = 8;
+// Parts of a block's dh sum over the vocabulary, as in the LM head's backward: dh's few tiles have
+// long sums, and the launch waits for them while they fill only some of the units. At most as
+// many as give every unit a part; none shorter than four slices of 64; and, as a slice takes
+// kSliceUs where few tiles run and a part is written and read once more, no more than make
+// slices * kSliceUs / n + n * rows * d * 8 bytes at 4 TB/s least. (48 rows of V = 4000, d = 512:
+// the products 66 us in one part, 15 in 7, PARTSUS in 15.)
+constexpr double kSliceUs = 0.75;
+int64_t dh_parts(int64_t rows, int64_t d, int64_t V) {
+    const int64_t tiles =
+        ((rows + LmCfg::BM - 1) / LmCfg::BM) * ((d + LmCfg::BN - 1) / LmCfg::BN);
+    const int64_t by_units = kUnits / tiles, by_k = V / (LmCfg::BK * 4);
+    const double slices = (double)V / LmCfg::BK, add_us = (double)rows * (double)d * 8 / 4e6;
+    const int64_t best = (int64_t)sqrt(slices * kSliceUs / add_us);
+    const int64_t n = by_units < by_k ? by_units : by_k;
+    return n < best ? (n > 1 ? n : 1) : (best > 1 ? best : 1);
+}
 
 // Where a call's parts sit in the workspace (byte offsets, each 256-byte aligned).
 struct XentPlan {
@@ -482,7 +520,7 @@ XentPlan plan_xent(int64_t T, int64_t d, int64_t V, int64_t rows, bool grad, boo
     XentPlan P = {};
     P.rows = rows < T ? rows : T;
     P.acc_w = grad && want_w && P.rows < T;
-    P.ksplit = grad ? lmhead::dh_parts(P.rows, d, V, kMinPartSlices) : 1;
+    P.ksplit = grad ? dh_parts(P.rows, d, V) : 1;
     const double big = double(int64_t(1) << 60), nvt = (double)vocab_tiles(V);
     if ((double)P.rows * (double)ceil8(V) * 2 > big || (double)V * (double)d * 4 > big ||
         (double)T * (double)d * 2 > big || (double)P.rows * nvt * 16 > big)
@@ -521,6 +559,20 @@ bool bad_inputs(const void* hidden, int64_t T, int64_t d, int64_t ld_h, const vo
         return true;
     if (d % 8 || ld_h < d || ld_w < d || ld_h % 8 || ld_w % 8) return true;
     return reinterpret_cast<uintptr_t>(hidden) % 16 || reinterpret_cast<uintptr_t>(weight) % 16;
+}
+
+// f(threads of a row's workgroup): about 16 vectors of eight columns each, which take turns with
+// the row's other latencies. 1220 rows of V = 1088: 16 us with 512, ROWSUS with 64.
+template <class F>
+void with_row_threads(int64_t V, F&& f) {
+    if (V <= 2048)
+        f(std::integral_constant<int, 64>{});
+    else if (V <= 8192)
+        f(std::integral_constant<int, 128>{});
+    else if (V <= 32768)
+        f(std::integral_constant<int, 256>{});
+    else
+        f(std::integral_constant<int, 512>{});
 }
 
 // The whole call; without grads the loss alone.
@@ -568,6 +620,10 @@ dart_status_t run_xent(const uint16_t* h, int64_t T, int64_t d, int64_t ld_h, co
     const Grad dh{grads ? grads->dh : nullptr, grads ? grads->ld_dh : 0, true};
     const Grad dw{grads ? grads->dw : nullptr, grads ? grads->ld_dw : 0, true};
     const Grad sum_w = P.acc_w ? Grad{ws + P.accw, d, false} : dw;
+    auto launch_finish = [&](int64_t blocks, float* to, const DhParts& to_add) {
+        hipLaunchKernelGGL(xent_finish_kernel, dim3((unsigned)(blocks + (to ? 1 : 0))),
+                           dim3(kFinishThreads), 0, stream, tok_loss, T, mean, count, to, to_add);
+    };
     for (int64_t r0 = 0; r0 < T; r0 += P.rows) {
         const int64_t rows = T - r0 < P.rows ? T - r0 : P.rows;
         const uint16_t* hr = h_c + r0 * d;
@@ -589,21 +645,28 @@ dart_status_t run_xent(const uint16_t* h, int64_t T, int64_t d, int64_t ld_h, co
                                tok_loss, count, r0);
             continue;
         }
-        hipLaunchKernelGGL((xent_rows_kernel<512, true>), dim3((unsigned)rows), dim3(512), 0, stream,
-                           part, reinterpret_cast<const float*>(unit_m), z_y, nvt, V, target_c + r0,
-                           map + r0, terms, e, ld_e, tok_loss, count, r0);
+        with_row_threads(V, [&](auto threads) {
+            constexpr int N = decltype(threads)::value;
+            hipLaunchKernelGGL((xent_rows_kernel<N, true>), dim3((unsigned)rows), dim3(N), 0, stream,
+                               part, reinterpret_cast<const float*>(unit_m), z_y, nvt, V,
+                               target_c + r0, map + r0, terms, e, ld_e, tok_loss, count, r0);
+        });
         const dart_status_t st = lmhead::launch_bwd_gemms(
             e, ld_e, rows, V, w, ld_w, hr, d, d, parts && dh.p ? Grad{parts, d, false} : dh, false,
             parts ? P.ksplit : 1, P.rows * d, sum_w, P.acc_w && r0 > 0, stream, parts ? nullptr : map + r0,
             count, r0, scale);
         if (st != DART_OK) return st;
+        const DhParts to_add = {parts, P.ksplit, P.rows * d, rows, d, map + r0, dh_rows, ld_dh, r0};
+        const bool last = r0 + rows == T;
+        const int64_t blocks = (rows * d / 4 + kFinishThreads - 1) / kFinishThreads;
         if (parts && dh.p)
-            lmhead::launch_sum_parts(parts, P.ksplit, P.rows * d, rows, d, map + r0, dh, count, r0,
-                                     stream);
+            launch_finish(blocks < kRowBlocksMost ? blocks : kRowBlocksMost, last ? loss : nullptr,
+                          to_add);
+        else if (last)
+            launch_finish(0, loss, to_add);
     }
     if (P.acc_w) lmhead::launch_to_bf16(reinterpret_cast<float*>(ws + P.accw), V, d, dw, stream);
-    hipLaunchKernelGGL(xent_loss_kernel, dim3(1), dim3(kLossThreads), 0, stream, tok_loss, T, mean,
-                       count, loss);
+    if (!grads) launch_finish(0, loss, DhParts{});
     return hipGetLastError() == hipSuccess ? DART_OK : DART_ERR_HIP;
 }
 
