@@ -704,8 +704,8 @@ dart_status_t dart_mxfp4_matmul(const void* a, int64_t M, const void* b, int64_t
  *              (T * ceil(V/128) * 16 + T * 4), 16-byte aligned, owned by the
  *              caller; contents on entry do not matter.
  * Errors: INVALID_ARG as dart_lmhead_tok_stats_ex and for a null or misaligned
- * quantised matrix; UNSUPPORTED when ceil(T/256) * ceil(V/128) exceeds 16,777,215,
- * T 67,108,860 or d 16,777,216; HIP when a launch fails. */
+ * quantised matrix; UNSUPPORTED when ceil(T/256) * ceil(V/128)
+ * or T exceeds 16,777,215 or d 16,777,216; HIP when a launch fails. */
 dart_status_t dart_lmhead_mxfp4_tok_stats(const void* hidden, int64_t T, const void* weight,
                                           int64_t V, int64_t d, const int32_t* target,
                                           float inv_temp, float* logp, float* entropy, float* lse,

@@ -501,10 +501,10 @@ __device__ __forceinline__ void bwd_gemm_tile(const BwdGemm& g, int64_t b, typen
         if (kbeg >= K && ACC) return;
     }
     const int64_t m0 = mt * C::BM, n0 = nt * C::BN;
+    const float f = g.scale ? *g.scale : 1.f;  // here, where its latency is hidden
     f32x16 acc[C::TM][C::TN];
     gemm_tile_bwd<C, A_KMAJ>(g.A, g.lda, g.B, g.ldb, M, N, kbeg, K, m0, n0, sm, acc);
     if (g.scale) {
-        const float f = *g.scale;
 #pragma unroll
         for (int i = 0; i < C::TM; ++i)
 #pragma unroll

@@ -559,7 +559,7 @@ __device__ __forceinline__ void stats_of_tile(F&& tile, int64_t T, int64_t V,
 #pragma unroll
                         for (int v = 0; v < 16; ++v) {
                             float xl = fmaf(acc[i][2 * u + j][v], c2, -ml);
-                            if constexpr (decltype(floored)::value) xl = fmaxf(xl, -200.f);
+                            if constexpr (decltype(floored)::value) xl = xl < -200.f ? -200.f : xl;
                             const float e = __builtin_amdgcn_exp2f(xl);
                             s2[j] += e;
                             w2[j] = fmaf(e, xl, w2[j]);

@@ -515,6 +515,51 @@ mxfp4_stats_kernel(Mxfp4Pair x, int64_t T, int64_t V, const int32_t* __restrict_
     });
 }
 
+// One workgroup per row: the row's nvt triples merged in index order by thread, lane and wave, and
+// the target logit last, as lmhead_merge_kernel does, whose single wave a row took 9 us for 64
+// rows of V = 152064 (1188 triples each), where this takes 6 (17 and 19 for 4096). A NaN among
+// the logits shows in the row's results.
+constexpr int kMergeThreads = 256;
+__global__ void __launch_bounds__(kMergeThreads)
+mxfp4_merge_kernel(const float4* __restrict__ part, const float* __restrict__ z_y, int64_t nvt,
+                   int64_t V, const int32_t* __restrict__ target, float* __restrict__ logp,
+                   float* __restrict__ entropy, float* __restrict__ lse) {
+    __shared__ Triple waves[kMergeThreads / 64];
+    const int64_t t = blockIdx.x;
+    const int tid = threadIdx.x, lane = tid & 63;
+    const int32_t y = target[t];
+    const float zy = y >= 0 && y < V ? z_y[t] : __builtin_nanf("");
+    Triple acc = {-INFINITY, 0.f, 0.f};
+    for (int64_t j0 = tid; j0 < nvt; j0 += kMergeThreads * kMergeBatch) {
+        float4 p[kMergeBatch];
+#pragma unroll
+        for (int k = 0; k < kMergeBatch; ++k) {
+            const int64_t j = j0 + kMergeThreads * k;
+            p[k] = j < nvt ? part[t * nvt + j] : make_float4(-INFINITY, 0.f, 0.f, 0.f);
+        }
+#pragma unroll
+        for (int k = 0; k < kMergeBatch; ++k) acc = merge(acc, Triple{p[k].x, p[k].y, p[k].z});
+    }
+#pragma unroll
+    for (int off = 32; off >= 1; off >>= 1)
+        acc = merge(acc, Triple{__shfl_xor(acc.m, off), __shfl_xor(acc.s, off),
+                                __shfl_xor(acc.w, off)});
+    if (lane == 0) waves[tid >> 6] = acc;
+    __syncthreads();
+    if (tid) return;
+#pragma unroll
+    for (int k = 1; k < kMergeThreads / 64; ++k) acc = merge(acc, waves[k]);
+    const bool others = acc.s != 0.f;  // also where it is a NaN
+    const float M = others ? fmaxf(acc.m, zy) : zy, dx = acc.m - M;
+    const float cx = others ? expf(dx) : 0.f;
+    const float sx = others ? cx * acc.s : 0.f, wx = others ? cx * fmaf(dx, acc.s, acc.w) : 0.f;
+    const float xy = zy - M, ey = expf(xy), S = sx + ey, ln_s = logf(S);
+    const float h = ln_s - fmaf(ey, xy, wx) / S;
+    lse[t] = M + ln_s;
+    entropy[t] = h < 0.f ? 0.f : h;
+    logp[t] = sx < ey ? -log1pf(sx / ey) : xy - ln_s;
+}
+
 // out = A B^T for up to 32 rows of A (one row of panels): the workgroup takes 32 rows of B, its
 // waves panels w, w + 4, ... of both, kInFlight at a time all loaded before the first is
 // multiplied; the waves' sums are added in order through LDS. No LDS on the way in: a panel of
@@ -704,7 +749,7 @@ dart_status_t dart_lmhead_mxfp4_tok_stats(const void* hidden, int64_t T, const v
         return DART_ERR_INVALID_ARG;
     const int64_t nvt = column_tiles(V);
     if (!grid_fits((T + Mx256::BM - 1) / Mx256::BM * nvt, Mx256::THREADS) ||
-        !grid_fits((T + kMergeWaves - 1) / kMergeWaves, kMergeWaves * 64) || d > kMaxK)
+        !grid_fits(T, kMergeThreads) || d > kMaxK)
         return DART_ERR_UNSUPPORTED;
     if (const dart_status_t ck = dart_check::run(
             stream, {{dart_check::Item::Ids, target, T, V}}); ck != DART_OK)
@@ -717,9 +762,8 @@ dart_status_t dart_lmhead_mxfp4_tok_stats(const void* hidden, int64_t T, const v
         hipLaunchKernelGGL(mxfp4_stats_kernel<C>, dim3((unsigned)((T + C::BM - 1) / C::BM * nvt)),
                            dim3(C::THREADS), 0, stream, x, T, V, target, inv_temp, nvt, part, z_y);
     });
-    hipLaunchKernelGGL(lmhead_merge_kernel, dim3((unsigned)((T + kMergeWaves - 1) / kMergeWaves)),
-                       dim3(kMergeWaves * 64), 0, stream, part, z_y, T, nvt, V, target, logp,
-                       entropy, lse);
+    hipLaunchKernelGGL(mxfp4_merge_kernel, dim3((unsigned)T), dim3(kMergeThreads), 0, stream, part,
+                       z_y, nvt, V, target, logp, entropy, lse);
     return hipGetLastError() == hipSuccess ? DART_OK : DART_ERR_HIP;
 }
 

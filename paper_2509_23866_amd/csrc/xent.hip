@@ -239,8 +239,10 @@ xent_rows_kernel(const float4* __restrict__ part, const float* __restrict__ unit
     __shared__ RowSums waves[WAVES];
     const int tid = threadIdx.x, lane = tid & 63;
     const int64_t r = blockIdx.x;
+    // (the row's own values all at once: they exist also past the labelled rows)
+    const int32_t y = target[r], row_to = map[r];
+    const float zy = z_y[r];
     if (r >= (int64_t)*n_rows - base) return;
-    const int32_t y = target[r];
     const int64_t chunks = (V + 7) / 8;
     [[maybe_unused]] u32x4* row = KEEP ? reinterpret_cast<u32x4*>(e + r * ld_e) : nullptr;
     RowSums x = {-INFINITY, 0.f, 0.0};
@@ -261,7 +263,6 @@ xent_rows_kernel(const float4* __restrict__ part, const float* __restrict__ unit
         for (int k = 1; k < WAVES; ++k) x = joined(x, waves[k]);
     }
     // the target last: lse = M + log S, logp from -log1p(s_rest / e_y) when it dominates
-    const float zy = z_y[r];
     // (x.s is 0 where there is no other column, a NaN where a logit is none)
     const float M = x.s != 0.f ? fmaxf(x.m, zy) : zy;
     const float sx = x.s != 0.f ? x.s * expf(x.m - M) : 0.f, ey = expf(zy - M);
@@ -271,7 +272,7 @@ xent_rows_kernel(const float4* __restrict__ part, const float* __restrict__ unit
         const double l = (double)lse;
         double loss = -(double)logp * (1.0 - (double)terms.eps) + (double)terms.lambda * l * l;
         if (terms.eps > 0.f) loss += (double)terms.eps * (l - x.z / (double)V);
-        tok_loss[map[r]] = (float)loss;
+        tok_loss[row_to] = (float)loss;
     }
     if constexpr (KEEP) {
         const float keep = 1.f / (1.f - terms.eps), g = 1.f + 2.f * terms.lambda * lse;

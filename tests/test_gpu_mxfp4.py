@@ -240,6 +240,25 @@ def test_tok_stats_shapes(T, d, V, inv_temp):
         assert np.array_equal(g.cpu().numpy(), a.cpu().numpy())
 
 
+def test_tok_stats_of_blocks_that_are_not_finite():
+    """A NaN block of a hidden row shows in that row alone, one of a weight row in every row."""
+    import torch
+
+    dart = _dart()
+    rng = np.random.default_rng(11)
+    h, w = rng.normal(size=(70, 96)), rng.normal(size=(400, 96))
+    y = _cuda(rng.integers(0, 399, 70).astype(np.int32))
+    qw = dart.dart_mxfp4_quantize(_cuda(w.astype(np.float32)))
+    h[5, 40] = np.nan
+    got = dart.dart_lmhead_mxfp4_tok_stats(_cuda(h.astype(np.float32)), qw, y)
+    for g in got:
+        assert torch.nonzero(g.isnan())[:, 0].tolist() == [5]
+    h[5, 40], w[399, 3] = 0.0, np.inf
+    qw = dart.dart_mxfp4_quantize(_cuda(w.astype(np.float32)))
+    for g in dart.dart_lmhead_mxfp4_tok_stats(_cuda(h.astype(np.float32)), qw, y):
+        assert bool(g.isnan().all())
+
+
 def test_tok_stats_do_not_depend_on_the_batch():
     """A row's statistics are the same bits alone, in a small and in a large call."""
     import torch
