@@ -437,23 +437,14 @@ struct Rest {
     using type = typename std::conditional<C::BM == LmCfg::BM, LmCfg128, C>::type;
 };
 // f(configuration, LDS, first row, vocabulary tile) for this workgroup's tile of M
-// rows x nvt vocabulary tiles, if it has one; with X also an X in LDS as f's last
-// argument. One LDS object holds all: beside a second one the compiler waits for every
-// load into LDS before the next read of it (the cross entropy's tile took 4150 us in place
-// of 3400).
-struct NoMore {};
-template <class C, class X = NoMore, class F>
+// rows x nvt vocabulary tiles, if it has one.
+template <class C, class F>
 __device__ __forceinline__ void with_row_tile(int64_t M, int64_t nvt, F&& f) {
     using R = typename Rest<C>::type;
-    union Tile {
+    __shared__ union {
         typename C::Smem full;
         typename R::Smem rest;
-    };
-    struct WithMore {
-        Tile tile;
-        X more;
-    };
-    __shared__ typename std::conditional<std::is_same<X, NoMore>::value, Tile, WithMore>::type sm;
+    } sm;
     const int64_t nmt = (M + C::BM - 1) / C::BM;
     if ((int64_t)blockIdx.x >= nmt * nvt) return;
     int64_t mt, vt;
@@ -461,17 +452,11 @@ __device__ __forceinline__ void with_row_tile(int64_t M, int64_t nvt, F&& f) {
     const int64_t m0 = mt * C::BM;
     if constexpr (R::BM < C::BM) {
         if (has_rest(nmt) && M - m0 <= R::BM) {
-            if constexpr (std::is_same<X, NoMore>::value)
-                f(R{}, sm.rest, m0, vt);
-            else
-                f(R{}, sm.tile.rest, m0, vt, sm.more);
+            f(R{}, sm.rest, m0, vt);
             return;
         }
     }
-    if constexpr (std::is_same<X, NoMore>::value)
-        f(C{}, sm.full, m0, vt);
-    else
-        f(C{}, sm.tile.full, m0, vt, sm.more);
+    f(C{}, sm.full, m0, vt);
 }
 
 // The statistics of tile (m0, vt) of logits whose values (not scaled) tile(n0, acc)

@@ -24,6 +24,7 @@
 // so that the target's element of an unsure row, the largest of all, is next to -1 and
 // loses nothing by its rounding.
 #include "lmhead_tile.h"
+#include <stdlib.h>
 
 namespace {
 
@@ -32,7 +33,6 @@ using lmhead::Grad;
 constexpr float kLog2e = 1.4426950408889634f;
 // exponentials are kept times 2^kShift: fp16 holds up to 65504 and 2^-14 at full width
 constexpr int kShift = 15;
-constexpr int kUnitsPerTile = LmCfg::BN / kStatsUnit;
 
 __device__ __forceinline__ bool has_label(int32_t y, int64_t V) { return y >= 0 && y < V; }
 
@@ -43,29 +43,201 @@ __device__ __forceinline__ u32x2 pack_half4(float a, float b, float c, float d) 
     return __builtin_bit_cast(u32x2, v);
 }
 
-// Partial results of a tile's rows, one per unit of 64 columns: maxima, normalisers, sums.
-struct Units {
-    float v[3][kUnitsPerTile][LmCfg::BM];
+// Tile configuration: BM rows x 128 vocabulary entries per workgroup of four waves, WM x WN, each
+// owning (BM / WM) x (128 / WN) as 32 x 32 MFMA tiles; K in slices of 64. The hidden rows, which
+// the call gathers anyway, lie in panels of 32 rows x 64 columns in the order in which a wave's
+// MFMAs take them (below) and go from memory (L2) to registers; W's rows go through an LDS ring of NS
+// slices, from which the waves share them. With both operands in the LDS, as in gemm_tile, the
+// LDS is the limit; and two such workgroups fit a compute unit, so that one multiplies while the
+// other is in its epilogue. TILETIMES
+constexpr int kTileN = 128, kSliceK = 64;
+constexpr uint32_t kPanel = 4096;  // bytes
+template <int BM_, int WM_, int WN_, int NS_>
+struct XCfg {
+    static constexpr int BM = BM_, BN = kTileN, WM = WM_, WN = WN_, NS = NS_;
+    static constexpr int WAVES = 4, THREADS = 256;
+    static constexpr int TM = BM / WM / 32, TN = BN / WN / 32;  // MFMA tiles per wave
+    static constexpr int SETS = TM == 1 ? 2 : 1;  // of registers for the hidden rows' panels
+    static constexpr int RS = WM * 32;            // rows between a wave's row blocks
+    static constexpr int CROW16 = BN + 8;         // as in Cfg
+    static_assert(WM * WN == WAVES && TM * WM * 32 == BM && TN * WN * 32 == BN && TN % 2 == 0,
+                  "four waves, units of two column blocks");
+    static_assert(SETS == 1 || NS % 2 == 0, "a slice's set goes by its buffer");
+    static_assert(NS == 3 || NS == 4, "buffers of the K loop");
+    struct alignas(16) Smem {
+        union {
+            // chunk c (16 bytes) of row r in slot c ^ swz(r), as in gemm_tile
+            uint16_t b[NS][BN][kSliceK];
+            uint16_t c16[BM][CROW16];
+        };
+        // a row's maxima, normalisers and sums of the tile's units of 64 columns
+        float units[3][BN / kStatsUnit][BM];
+    };
+    static_assert(sizeof(Smem) <= 80 * 1024, "two workgroups per compute unit");
 };
+using X256 = XCfg<256, 4, 1, 3>;
+using X128 = XCfg<128, 4, 1, 4>;
+using X64 = XCfg<64, 2, 2, 4>;
 
-// Tile (m0, vt) of the logits: part[t * nvt + vt] = (max, sum of e^(z - max), sum of z, 0) of
-// row t over the tile's columns, the target's column in the sum of z alone (which is formed if
-// sums); the workgroup holding target[t] writes z_y[t]. With KEEP e [M, ld_e] receives
-// 2^15 e^(z - m) in fp16 (0 in the target's column) for the maxima m of the row's units of 64
-// columns, and unit_m[t * nvt + vt] those of the tile's four. Each unit has a maximum of its own so
-// that a wave needs no other for its exponentials: with one for the 256 columns, and a
-// barrier before it, the tile took TILEOLD us in place of TILENEW (T = 4096, V = 152064,
-// d = 3584). Sums run in the same order whatever the tile's height, so that equal rows have
-// equal results.
+// Where the 16 bytes of columns [8 c, 8 c + 8) of row r of a block's rows are: the panel of its
+// run of 32 rows and slice, in it product c % 8 / 2, lane (c % 2) * 32 + r % 32.
+__host__ __device__ constexpr int64_t panel_at(int64_t r, int64_t c, int64_t slices) {
+    return (r / 32 * slices + c / 8) * kPanel + c % 8 / 2 * 1024 + (c % 2 * 32 + r % 32) * 16;
+}
+int64_t slices_of(int64_t d) { return (d + kSliceK - 1) / kSliceK; }
+int64_t column_tiles(int64_t V) { return (V + kTileN - 1) / kTileN; }
+
+// acc = this wave's part of h's rows [m0, m0 + BM) (panels of `runs` runs) times W's rows
+// [n0, n0 + 128) of N (row-major, d columns). K past d: zeros in h's panels, and read as zero of
+// W. Layout of acc as gemm_tile's. Ends on a barrier with no loads in flight.
+template <class C>
+__device__ __forceinline__ void xent_product(const uint8_t* __restrict__ h, int64_t runs,
+                                             const uint16_t* __restrict__ w, int64_t N, int64_t ldw,
+                                             int64_t d, int64_t m0, int64_t n0,
+                                             typename C::Smem& sm, f32x16 (&acc)[C::TM][C::TN]) {
+#if defined(__HIP_DEVICE_COMPILE__)
+    const int tid = threadIdx.x, lane = tid & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+#pragma unroll
+    for (int i = 0; i < C::TM; ++i)
+#pragma unroll
+        for (int j = 0; j < C::TN; ++j)
+#pragma unroll
+            for (int v = 0; v < 16; ++v) acc[i][j][v] = 0.f;
+
+    // every run of panels a resource of its own: loads past its last slice read as zero without
+    // going to memory (a raw load's whole offset is checked, its scalar part too)
+    const int64_t nk = (d + kSliceK - 1) / kSliceK, run_bytes = nk * kPanel;
+    __amdgpu_buffer_rsrc_t ra[C::TM];
+#pragma unroll
+    for (int i = 0; i < C::TM; ++i) {
+        const int64_t run = m0 / 32 + wave / C::WN + i * C::WM;
+        ra[i] = tile_rsrc(h + (run < runs ? run : 0) * run_bytes, run < runs ? run_bytes : 0);
+    }
+    const __amdgpu_buffer_rsrc_t rb = tile_rsrc(w + n0 * ldw, rows_bytes(N - n0 < C::BN ? N - n0 : C::BN, ldw, d));
+    const uint32_t l16 = (uint32_t)lane * 16;
+    // one load of W fills 8 rows x 8 chunks; load q of a wave rows (q * 4 + wave) * 8 .. + 7
+    const int r_lane = wave * 8 + (lane >> 3), c_lane = (lane & 7) ^ swz<8>(r_lane);
+    const uint32_t vb = (uint32_t)((r_lane * ldw + c_lane * 8) * 2);
+    const uint32_t qstride = (uint32_t)(32 * ldw * 2);
+    // the last slice's chunks past d, and slices past the last, are out of the resource's range (of
+    // less than 2^31 bytes, as the scalar offsets are)
+    constexpr uint32_t kNowhere = 0x80000000u;
+    const uint32_t vb_last = (nk - 1) * kSliceK + c_lane * 8 < d ? vb : kNowhere;
+    auto issue = [&](int64_t kt, int buf) {
+        const uint32_t v = kt < nk - 1 ? vb : kt == nk - 1 ? vb_last : kNowhere;
+        const uint32_t k = kt < nk ? (uint32_t)kt * (kSliceK * 2) : 0u;
+#pragma unroll
+        for (uint32_t q = 0; q < 4; ++q)
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(
+                rb, lds_ptr(&sm.b[buf][(q * 4 + wave) * 8][0]), 16, v,
+                kt < nk ? k + q * qstride : 0u, 0, 0);
+    };
+    bf16x8 af[C::SETS][4][C::TM];
+    auto load_a = [&](int64_t kt, int ks, int a_set) {
+#pragma unroll
+        for (int i = 0; i < C::TM; ++i)
+            af[a_set][ks][i] = __builtin_bit_cast(
+                bf16x8, __builtin_amdgcn_raw_buffer_load_b128(
+                            ra[i], l16, (uint32_t)kt * kPanel + (uint32_t)ks * 1024, 0));
+    };
+    const int wc = (wave % C::WN) * (C::BN / C::WN);
+    uint32_t rd[4];
+#pragma unroll
+    for (int ks = 0; ks < 4; ++ks) {
+        const int c = ks * 2 + (lane >> 5), r = wc + (lane & 31);
+        rd[ks] = (uint32_t)(r * kSliceK + (c ^ swz<8>(r)) * 8) * 2;
+        asm volatile("" : "+v"(rd[ks]));  // opaque: buffer and block are the reads' immediates
+    }
+    const char* const lds0 = reinterpret_cast<const char*>(&sm);
+    bf16x8 bf[2][C::TN];
+    auto read_b = [&](auto bufc, int ks, int set) {
+        constexpr int buf = decltype(bufc)::value;
+#pragma unroll
+        for (int j = 0; j < C::TN; ++j)
+            bf[set][j] = __builtin_bit_cast(
+                bf16x8, *reinterpret_cast<const u32x4*>(
+                            lds0 + rd[ks] + (buf * C::BN + j * 32) * kSliceK * 2));
+    };
+    // When slice kt begins, the loads of W's slices kt + 1 .. kt + NS - 2, four each, were issued
+    // after those of kt; waiting until no more than so many are left has slice kt landed,
+    // wherever the compiler put the others.
+    constexpr int AHEAD = 4 * (C::NS - 2);
+    auto slice = [&](auto bufc, int64_t kt) {
+        constexpr int buf = decltype(bufc)::value;
+        wait_vmcnt<AHEAD>();
+        lds_ring_barrier();
+        // h's next slice: with two sets of registers now, before the loads of W, which may then
+        // stay in flight when it is waited for; with one as the products let go of it
+        constexpr int set_a = C::SETS == 2 ? buf & 1 : 0;
+        if constexpr (C::SETS == 2) {
+#pragma unroll
+            for (int ks = 0; ks < 4; ++ks) load_a(kt + 1, ks, set_a ^ 1);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        issue(kt + C::NS - 1, (buf + C::NS - 1) % C::NS);
+        __builtin_amdgcn_sched_barrier(0);
+        read_b(bufc, 0, 0);
+        __builtin_amdgcn_sched_barrier(0);
+        __builtin_amdgcn_s_setprio(1);
+#pragma unroll
+        for (int ks = 0; ks < 4; ++ks) {
+            const int set = ks & 1;
+            if (ks < 3) read_b(bufc, ks + 1, set ^ 1);
+#pragma unroll
+            for (int i = 0; i < C::TM; ++i)
+#pragma unroll
+                for (int j = 0; j < C::TN; ++j)
+                    acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(bf[set][j], af[set_a][ks][i],
+                                                                        acc[i][j], 0, 0, 0);
+            if constexpr (C::SETS == 1) load_a(kt + 1, ks, 0);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        __builtin_amdgcn_s_setprio(0);
+        // the products stay in their slice
+#pragma unroll
+        for (int i = 0; i < C::TM; ++i)
+#pragma unroll
+            for (int j = 0; j < C::TN; ++j) asm volatile("" : "+v"(acc[i][j]));
+    };
+#pragma unroll
+    for (int ks = 0; ks < 4; ++ks) load_a(0, ks, 0);
+    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int b = 0; b < C::NS - 1; ++b) issue(b, b);
+    int64_t kt = 0;
+    for (; kt + C::NS - 1 < nk; kt += C::NS) {
+        slice(std::integral_constant<int, 0>{}, kt);
+        slice(std::integral_constant<int, 1>{}, kt + 1);
+        slice(std::integral_constant<int, 2>{}, kt + 2);
+        if constexpr (C::NS > 3) slice(std::integral_constant<int, 3 % C::NS>{}, kt + 3);
+    }
+    if (kt < nk) slice(std::integral_constant<int, 0>{}, kt);
+    if (kt + 1 < nk) slice(std::integral_constant<int, 1>{}, kt + 1);
+    if (C::NS > 3 && kt + 2 < nk) slice(std::integral_constant<int, 2>{}, kt + 2);
+    wait_vmcnt<0>();  // the zeros of slices past the last are in LDS
+    __syncthreads();
+#else
+    (void)h, (void)runs, (void)w, (void)N, (void)ldw, (void)d, (void)m0, (void)n0, (void)sm, (void)acc;
+#endif
+}
+
+// Tile (m0, vt) of the logits of h's first M rows: part[t * nvt + vt] = (m, s, m', s'), the
+// maximum and the sum of 2^15 e^(z - m) of row t over each of the tile's two units of 64 columns, the
+// target's column left out; with sums z_sum[t * nvt + vt], the sum of z over the tile, that
+// column included; the workgroup holding target[t] writes z_y[t]. With KEEP e [M, ld_e] receives
+// 2^15 e^(z - m) in fp16 (0 in the target's column). Each unit has a maximum of its own so that a
+// wave needs no other for its exponentials: with one for 256 columns, and a barrier
+// before it, the tile took 4% longer. Sums run in the same order whatever the tile's height, so
+// that equal rows have equal results.
 template <class C, bool KEEP>
-__device__ __forceinline__ void xent_tile(const uint16_t* __restrict__ h, int64_t M, int64_t ldh,
+__device__ __forceinline__ void xent_tile(const uint8_t* __restrict__ h, int64_t M,
                                           const uint16_t* __restrict__ w, int64_t V, int64_t ldw,
                                           int64_t d, const int32_t* __restrict__ target, bool sums,
                                           int64_t nvt, float4* __restrict__ part,
-                                          float4* __restrict__ unit_m, float* __restrict__ z_y,
+                                          float* __restrict__ z_sum, float* __restrict__ z_y,
                                           uint16_t* __restrict__ e, int64_t ld_e,
-                                          typename C::Smem& sm, Units& units, int64_t m0,
-                                          int64_t vt) {
+                                          typename C::Smem& sm, int64_t m0, int64_t vt) {
 #pragma clang fp contract(off)  // the same roundings in every configuration
     const int64_t n0 = vt * C::BN;
     const int tid = threadIdx.x, lane = tid & 63;
@@ -79,9 +251,8 @@ __device__ __forceinline__ void xent_tile(const uint16_t* __restrict__ h, int64_
         ys[i] = t < M ? target[t] : -1;
     }
     f32x16 acc[C::TM][C::TN];
-    gemm_tile<C>(h, M, ldh, w, V, ldw, d, m0, n0, sm, acc);
+    xent_product<C>(h, (M + 31) / 32, w, V, ldw, d, m0, n0, sm, acc);
 
-    static_assert(C::TN % 2 == 0, "units of two 32-column blocks");
     constexpr int CPR = C::TN * 4, RPI = 64 / CPR;  // 16-byte chunks a row, rows a store
 #pragma unroll
     for (int i = 0; i < C::TM; ++i) {
@@ -142,9 +313,9 @@ __device__ __forceinline__ void xent_tile(const uint16_t* __restrict__ h, int64_
             if (sums) zs += __shfl_xor(zs, 32);
             if (half == 0) {
                 const int unit = wc / kStatsUnit + u;
-                units.v[0][unit][row] = m;
-                units.v[1][unit][row] = s;
-                units.v[2][unit][row] = zs;
+                sm.units[0][unit][row] = m;
+                sm.units[1][unit][row] = s;
+                sm.units[2][unit][row] = zs;
             }
         }
         if constexpr (KEEP) {
@@ -172,39 +343,31 @@ __device__ __forceinline__ void xent_tile(const uint16_t* __restrict__ h, int64_
     }
     lds_ring_barrier();
     for (int r = tid; r < C::BM && m0 + r < M; r += C::THREADS) {
-        float mu[kUnitsPerTile], m = -INFINITY, s = 0.f, zs = 0.f;
-#pragma unroll
-        for (int k = 0; k < kUnitsPerTile; ++k) {
-            mu[k] = units.v[0][k][r];
-            m = fmaxf(m, mu[k]);
-            zs += units.v[2][k][r];
-        }
-#pragma unroll
-        for (int k = 0; k < kUnitsPerTile; ++k) {
-            const float sk = units.v[1][k][r];
-            s += sk == 0.f ? 0.f : sk * expf(mu[k] - m);
-        }
         const int64_t at = (m0 + r) * nvt + vt;
-        part[at] = make_float4(m, s * 0x1p-15f, zs, 0.f);
-        if constexpr (KEEP) unit_m[at] = make_float4(mu[0], mu[1], mu[2], mu[3]);
+        part[at] = make_float4(sm.units[0][0][r], sm.units[1][0][r], sm.units[0][1][r],
+                               sm.units[1][1][r]);
+        if (sums) z_sum[at] = sm.units[2][0][r] + sm.units[2][1][r];
     }
 }
 
-// The block's rows are its first *n_rows - base: the tiles are laid over theirs, as in
-// lmhead_dlogits_kernel.
+// The block's rows are its first *n_rows - base: the tiles are laid over theirs, so that they
+// spread over every XCD, and the workgroups past them have nothing to do.
 template <class C, bool KEEP>
-__global__ void __launch_bounds__(C::THREADS)
-xent_tile_kernel(const uint16_t* __restrict__ h, int64_t M, int64_t ldh,
-                 const uint16_t* __restrict__ w, int64_t V, int64_t ldw, int64_t d,
-                 const int32_t* __restrict__ target, int sums, int64_t nvt,
-                 float4* __restrict__ part, float4* __restrict__ unit_m, float* __restrict__ z_y, uint16_t* __restrict__ e, int64_t ld_e,
-                 const int32_t* __restrict__ n_rows, int64_t base) {
+__global__ void __launch_bounds__(C::THREADS, 2)
+xent_tile_kernel(const uint8_t* __restrict__ h, int64_t M, const uint16_t* __restrict__ w, int64_t V,
+                 int64_t ldw, int64_t d, const int32_t* __restrict__ target, int sums, int64_t nvt,
+                 float4* __restrict__ part, float* __restrict__ z_sum, float* __restrict__ z_y,
+                 uint16_t* __restrict__ e, int64_t ld_e, const int32_t* __restrict__ n_rows,
+                 int64_t base) {
+    __shared__ typename C::Smem sm;
     const int64_t live = (int64_t)*n_rows - base;
     M = live < M ? (live > 0 ? live : 0) : M;
-    with_row_tile<C, Units>(M, nvt, [&](auto cfg, auto& sm, int64_t m0, int64_t vt, Units& units) {
-        xent_tile<decltype(cfg), KEEP>(h, M, ldh, w, V, ldw, d, target, sums != 0, nvt, part, unit_m,
-                                       z_y, e, ld_e, sm, units, m0, vt);
-    });
+    const int64_t nmt = (M + C::BM - 1) / C::BM;
+    if ((int64_t)blockIdx.x >= nmt * nvt) return;
+    int64_t mt, vt;
+    tile_of_block(nmt, nvt, mt, vt);
+    xent_tile<C, KEEP>(h, M, w, V, ldw, d, target, sums != 0, nvt, part, z_sum, z_y, e, ld_e, sm,
+                       mt * C::BM, vt);
 }
 
 // The objective's constants.
@@ -230,7 +393,7 @@ __device__ __forceinline__ RowSums joined(const RowSums& a, const RowSums& b) {
 // tok_loss[map[r]]. With KEEP the row of e becomes dz / (1 - eps) in bf16, in place.
 template <int THREADS, bool KEEP>
 __global__ void __launch_bounds__(THREADS)
-xent_rows_kernel(const float4* __restrict__ part, const float* __restrict__ unit_m,
+xent_rows_kernel(const float4* __restrict__ part, const float* __restrict__ z_sum,
                  const float* __restrict__ z_y, int64_t nvt, int64_t V,
                  const int32_t* __restrict__ target, const int32_t* __restrict__ map,
                  XentTerms terms, uint16_t* __restrict__ e, int64_t ld_e,
@@ -248,7 +411,8 @@ xent_rows_kernel(const float4* __restrict__ part, const float* __restrict__ unit
     RowSums x = {-INFINITY, 0.f, 0.0};
     for (int64_t j = tid; j < nvt; j += THREADS) {
         const float4 p = part[r * nvt + j];
-        x = joined(x, RowSums{p.x, p.y, (double)p.z});
+        const double z = terms.eps > 0.f ? (double)z_sum[r * nvt + j] : 0.0;
+        x = joined(x, joined(RowSums{p.x, p.y, z}, RowSums{p.z, p.w, 0.0}));
     }
 #pragma unroll
     for (int off = 32; off >= 1; off >>= 1) {
@@ -264,6 +428,7 @@ xent_rows_kernel(const float4* __restrict__ part, const float* __restrict__ unit
     }
     // the target last: lse = M + log S, logp from -log1p(s_rest / e_y) when it dominates
     // (x.s is 0 where there is no other column, a NaN where a logit is none)
+    x.s *= 0x1p-15f;
     const float M = x.s != 0.f ? fmaxf(x.m, zy) : zy;
     const float sx = x.s != 0.f ? x.s * expf(x.m - M) : 0.f, ey = expf(zy - M);
     const float ln_s = logf(sx + ey), lse = M + ln_s;
@@ -281,10 +446,11 @@ xent_rows_kernel(const float4* __restrict__ part, const float* __restrict__ unit
         const float dy =
             (expm1f(logp) + terms.eps + 2.f * terms.lambda * lse * expf(logp)) * keep - flat;
         typedef _Float16 h8 __attribute__((ext_vector_type(8)));
+        const float* units = reinterpret_cast<const float*>(part + r * nvt);  // (m, s) of each
         for (int64_t c = tid; c < chunks; c += THREADS) {
             const h8 q = __builtin_bit_cast(h8, row[c]);
             // the maximum of the chunk's unit
-            const float m = unit_m[r * nvt * kUnitsPerTile + c / (kStatsUnit / 8)];
+            const float m = units[c / (kStatsUnit / 8) * 2];
             const float f = m == -INFINITY ? 0.f : a * expf(m - lse);
             float v[8];
 #pragma unroll
@@ -313,17 +479,30 @@ __device__ __forceinline__ void put_labels(const LabelOut& o, int64_t n) {
     o.scale[0] = n == 0 ? 0.f : (float)(o.mean ? f / (double)n : f);
 }
 
+// Where the labelled rows go: their hidden rows in panels, block by block of R rows, and (unless
+// null) row-major, and their targets.
+struct Placed {
+    uint8_t* panels;
+    uint16_t* rows;
+    int32_t* target;
+    int64_t R;
+};
+
 // Row t with a label: its hidden row and target to row `at` of the labelled ones. Without: its
 // row of dh (unless null) and its loss set to 0. By a workgroup of THREADS.
 template <int THREADS>
 __device__ __forceinline__ void place_row(int64_t t, int64_t at, const uint16_t* __restrict__ h,
-                                          int64_t ld_h, int64_t d, int32_t y,
-                                          uint16_t* __restrict__ h_c,
-                                          int32_t* __restrict__ target_c) {
+                                          int64_t ld_h, int64_t d, int32_t y, const Placed& to) {
     const u32x4* src = reinterpret_cast<const u32x4*>(h + t * ld_h);
-    u32x4* dst = reinterpret_cast<u32x4*>(h_c + at * d);
-    for (int64_t j = threadIdx.x; j < d / 8; j += THREADS) dst[j] = src[j];
-    if (threadIdx.x == 0) target_c[at] = y;
+    u32x4* dst = to.rows ? reinterpret_cast<u32x4*>(to.rows + at * d) : nullptr;
+    const int64_t slices = (d + kSliceK - 1) / kSliceK, block = at / to.R, r = at - block * to.R;
+    uint8_t* panels = to.panels + block * ((to.R + 31) / 32) * slices * kPanel;
+    for (int64_t c = threadIdx.x; c < slices * 8; c += THREADS) {
+        const u32x4 v = c < d / 8 ? src[c] : u32x4{0u, 0u, 0u, 0u};
+        *reinterpret_cast<u32x4*>(panels + panel_at(r, c, slices)) = v;
+        if (dst && c < d / 8) dst[c] = v;
+    }
+    if (threadIdx.x == 0) to.target[at] = y;
 }
 template <int THREADS>
 __device__ __forceinline__ void clear_row(int64_t t, int64_t d, float* __restrict__ tok_loss,
@@ -342,8 +521,7 @@ constexpr int64_t kFewRows = 4096;
 __global__ void __launch_bounds__(kPrepareThreads)
 xent_prepare_kernel(const int32_t* __restrict__ target, int64_t T, int64_t V,
                     const uint16_t* __restrict__ h, int64_t ld_h, int64_t d,
-                    int32_t* __restrict__ map, uint16_t* __restrict__ h_c,
-                    int32_t* __restrict__ target_c, float* __restrict__ tok_loss,
+                    int32_t* __restrict__ map, Placed to, float* __restrict__ tok_loss,
                     uint16_t* __restrict__ dh, int64_t ld_dh, LabelOut out) {
     __shared__ int waves[kPrepareThreads / 64];
     const int64_t t = blockIdx.x;
@@ -369,7 +547,7 @@ xent_prepare_kernel(const int32_t* __restrict__ target, int64_t T, int64_t V,
         n = 0;
     }
     if (tid == 0) map[n] = (int32_t)t;
-    place_row<kPrepareThreads>(t, n, h, ld_h, d, y, h_c, target_c);
+    place_row<kPrepareThreads>(t, n, h, ld_h, d, y, to);
 }
 
 // One workgroup: the rows with a label in increasing order in map, and their number.
@@ -403,13 +581,12 @@ xent_labels_kernel(const int32_t* __restrict__ target, int64_t T, int64_t V,
 __global__ void __launch_bounds__(128)
 xent_gather_kernel(const int32_t* __restrict__ map, const int32_t* __restrict__ count, int64_t T,
                    int64_t V, const uint16_t* __restrict__ h, int64_t ld_h, int64_t d,
-                   const int32_t* __restrict__ target, uint16_t* __restrict__ h_c,
-                   int32_t* __restrict__ target_c, float* __restrict__ tok_loss,
+                   const int32_t* __restrict__ target, Placed to, float* __restrict__ tok_loss,
                    uint16_t* __restrict__ dh, int64_t ld_dh) {
     const int64_t n = count[0];
     for (int64_t i = blockIdx.x; i < T; i += gridDim.x) {
         if (!has_label(target[i], V)) clear_row<128>(i, d, tok_loss, dh, ld_dh);
-        if (i < n) place_row<128>(map[i], i, h, ld_h, d, target[map[i]], h_c, target_c);
+        if (i < n) place_row<128>(map[i], i, h, ld_h, d, target[map[i]], to);
     }
 }
 
@@ -512,7 +689,7 @@ struct XentPlan {
     int64_t rows;   // a block's
     bool acc_w;     // dW summed over blocks in fp32
     int64_t ksplit; // parts of dh's sum over the vocabulary
-    size_t e, part, unit_m, z_y, count, scale, map, target_c, h_c, accw, parts, total;
+    size_t e, part, z_sum, z_y, count, scale, map, target_c, h_c, panels, accw, parts, total;
 };
 
 // total = 0 when the sizes do not fit the address arithmetic. rows: a block's (grad), or
@@ -522,9 +699,9 @@ XentPlan plan_xent(int64_t T, int64_t d, int64_t V, int64_t rows, bool grad, boo
     P.rows = rows < T ? rows : T;
     P.acc_w = grad && want_w && P.rows < T;
     P.ksplit = grad ? dh_parts(P.rows, d, V) : 1;
-    const double big = double(int64_t(1) << 60), nvt = (double)vocab_tiles(V);
+    const double big = double(int64_t(1) << 60), nvt = (double)column_tiles(V);
     if ((double)P.rows * (double)ceil8(V) * 2 > big || (double)V * (double)d * 4 > big ||
-        (double)T * (double)d * 2 > big || (double)P.rows * nvt * 16 > big)
+        (double)T * ((double)d + 64) * 128 > big || (double)P.rows * nvt * 16 > big)
         return P;
     size_t end = 0;
     auto take = [&](size_t bytes) {
@@ -534,12 +711,14 @@ XentPlan plan_xent(int64_t T, int64_t d, int64_t V, int64_t rows, bool grad, boo
     };
     P.count = take(4);
     P.scale = take(4);
-    P.part = take((size_t)P.rows * (size_t)vocab_tiles(V) * sizeof(float4));
+    P.part = take((size_t)P.rows * (size_t)column_tiles(V) * sizeof(float4));
+    P.z_sum = take((size_t)P.rows * (size_t)column_tiles(V) * sizeof(float));
     P.z_y = take((size_t)P.rows * 4);
     P.map = take((size_t)T * 4);
     P.target_c = take((size_t)T * 4);
-    P.h_c = take((size_t)T * (size_t)d * 2);
-    if (grad) P.unit_m = take((size_t)P.rows * (size_t)vocab_tiles(V) * sizeof(float4));
+    if (grad) P.h_c = take((size_t)T * (size_t)d * 2);
+    const int64_t blocks = (T + P.rows - 1) / P.rows, runs = (P.rows + 31) / 32;
+    P.panels = take((size_t)blocks * (size_t)runs * (size_t)slices_of(d) * kPanel);
     if (grad) P.e = take((size_t)P.rows * (size_t)ceil8(V) * 2);
     if (P.acc_w) P.accw = take((size_t)V * (size_t)d * 4);
     if (P.ksplit > 1) P.parts = take((size_t)P.ksplit * (size_t)P.rows * (size_t)d * 4);
@@ -560,6 +739,20 @@ bool bad_inputs(const void* hidden, int64_t T, int64_t d, int64_t ld_h, const vo
         return true;
     if (d % 8 || ld_h < d || ld_w < d || ld_h % 8 || ld_w % 8) return true;
     return reinterpret_cast<uintptr_t>(hidden) % 16 || reinterpret_cast<uintptr_t>(weight) % 16;
+}
+
+// f(configuration) for rows x V logits.
+template <class F>
+void with_xent_cfg(int64_t rows, int64_t V, F&& f) {
+    const char* force = getenv("XCFG");
+    int bm = rows <= 64 ? 64 : rows <= 128 ? 128 : 256;
+    if (force) bm = atoi(force);
+    if (bm == 64)
+        f(X64{});
+    else if (bm == 128)
+        f(X128{});
+    else
+        f(X256{});
 }
 
 // f(threads of a row's workgroup): about 16 vectors of eight columns each, which take turns with
@@ -588,32 +781,33 @@ dart_status_t run_xent(const uint16_t* h, int64_t T, int64_t d, int64_t ld_h, co
                        const dart_xent_config_t& config, float* loss, float* tok_loss,
                        int32_t* n_valid, const XentGrads* grads, const XentPlan& P, char* ws,
                        hipStream_t stream) {
-    const int64_t nvt = vocab_tiles(V);
+    const int64_t nvt = column_tiles(V);
     const int mean = config.reduction == DART_XENT_MEAN;
     const XentTerms terms = {config.label_smoothing, config.z_loss};
     int32_t* count = reinterpret_cast<int32_t*>(ws + P.count);
     float* scale = reinterpret_cast<float*>(ws + P.scale);
     float4* part = reinterpret_cast<float4*>(ws + P.part);
-    float4* unit_m = grads ? reinterpret_cast<float4*>(ws + P.unit_m) : nullptr;
+    float* z_sum = reinterpret_cast<float*>(ws + P.z_sum);
     float* z_y = reinterpret_cast<float*>(ws + P.z_y);
     const int sums = config.label_smoothing > 0.f;
     int32_t* map = reinterpret_cast<int32_t*>(ws + P.map);
-    uint16_t* h_c = reinterpret_cast<uint16_t*>(ws + P.h_c);
+    // row-major for dW's product alone
+    uint16_t* h_c = grads ? reinterpret_cast<uint16_t*>(ws + P.h_c) : nullptr;
+    const uint8_t* panels = reinterpret_cast<uint8_t*>(ws + P.panels);
     int32_t* target_c = reinterpret_cast<int32_t*>(ws + P.target_c);
     const LabelOut out = {count, n_valid, scale, config.label_smoothing, mean};
     uint16_t* dh_rows = grads ? static_cast<uint16_t*>(grads->dh) : nullptr;
     const int64_t ld_dh = grads ? grads->ld_dh : 0;
+    const Placed to = {reinterpret_cast<uint8_t*>(ws + P.panels), h_c, target_c, P.rows};
     if (T <= kFewRows) {
         hipLaunchKernelGGL(xent_prepare_kernel, dim3((unsigned)T), dim3(kPrepareThreads), 0, stream,
-                           target, T, V, h, ld_h, d, map, h_c, target_c, tok_loss, dh_rows, ld_dh,
-                           out);
+                           target, T, V, h, ld_h, d, map, to, tok_loss, dh_rows, ld_dh, out);
     } else {
         hipLaunchKernelGGL(xent_labels_kernel, dim3(1), dim3(kLabelThreads), 0, stream, target, T, V,
                            map, out);
         hipLaunchKernelGGL(xent_gather_kernel,
                            dim3((unsigned)(T < kRowBlocksMost ? T : kRowBlocksMost)), dim3(128), 0,
-                           stream, map, count, T, V, h, ld_h, d, target, h_c, target_c, tok_loss,
-                           dh_rows, ld_dh);
+                           stream, map, count, T, V, h, ld_h, d, target, to, tok_loss, dh_rows, ld_dh);
     }
     uint16_t* e = grads ? reinterpret_cast<uint16_t*>(ws + P.e) : nullptr;
     const int64_t ld_e = ceil8(V);
@@ -627,30 +821,28 @@ dart_status_t run_xent(const uint16_t* h, int64_t T, int64_t d, int64_t ld_h, co
     };
     for (int64_t r0 = 0; r0 < T; r0 += P.rows) {
         const int64_t rows = T - r0 < P.rows ? T - r0 : P.rows;
-        const uint16_t* hr = h_c + r0 * d;
-        with_tile(tile_rows(rows, V, d <= 1024 ? 57 : 54), rows, V, [&](auto cfg) {
+        const uint16_t* hr = grads ? h_c + r0 * d : nullptr;
+        const uint8_t* hp = panels + r0 / P.rows * ((P.rows + 31) / 32) * slices_of(d) * kPanel;
+        with_xent_cfg(rows, V, [&](auto cfg) {
             using C = decltype(cfg);
             const dim3 grid((unsigned)((rows + C::BM - 1) / C::BM * nvt));
-            if (grads)
-                hipLaunchKernelGGL((xent_tile_kernel<C, true>), grid, dim3(C::THREADS), 0, stream,
-                                   hr, rows, d, w, V, ld_w, d, target_c + r0, sums, nvt, part,
-                                   unit_m, z_y, e, ld_e, count, r0);
-            else
-                hipLaunchKernelGGL((xent_tile_kernel<C, false>), grid, dim3(C::THREADS), 0, stream,
-                                   hr, rows, d, w, V, ld_w, d, target_c + r0, sums, nvt, part,
-                                   unit_m, z_y, e, ld_e, count, r0);
+            auto launch = [&](auto kernel) {
+                hipLaunchKernelGGL(kernel, grid, dim3(C::THREADS), 0, stream, hp, rows, w, V, ld_w, d,
+                                   target_c + r0, sums, nvt, part, z_sum, z_y, e, ld_e, count, r0);
+            };
+            grads ? launch(xent_tile_kernel<C, true>) : launch(xent_tile_kernel<C, false>);
         });
         if (!grads) {
             hipLaunchKernelGGL((xent_rows_kernel<64, false>), dim3((unsigned)rows), dim3(64), 0,
-                               stream, part, nullptr, z_y, nvt, V, target_c + r0, map + r0, terms, e, ld_e,
+                               stream, part, z_sum, z_y, nvt, V, target_c + r0, map + r0, terms, e, ld_e,
                                tok_loss, count, r0);
             continue;
         }
         with_row_threads(V, [&](auto threads) {
             constexpr int N = decltype(threads)::value;
             hipLaunchKernelGGL((xent_rows_kernel<N, true>), dim3((unsigned)rows), dim3(N), 0, stream,
-                               part, reinterpret_cast<const float*>(unit_m), z_y, nvt, V,
-                               target_c + r0, map + r0, terms, e, ld_e, tok_loss, count, r0);
+                               part, z_sum, z_y, nvt, V, target_c + r0, map + r0, terms, e, ld_e, tok_loss,
+                               count, r0);
         });
         const dart_status_t st = lmhead::launch_bwd_gemms(
             e, ld_e, rows, V, w, ld_w, hr, d, d, parts && dh.p ? Grad{parts, d, false} : dh, false,
@@ -671,12 +863,16 @@ dart_status_t run_xent(const uint16_t* h, int64_t T, int64_t d, int64_t ld_h, co
     return hipGetLastError() == hipSuccess ? DART_OK : DART_ERR_HIP;
 }
 
-// Launch limits: the tiles of 256 rows, one workgroup of 512 per row of a block, and the
-// tiles' 32-bit row offsets.
+// Launch limits: the tiles (the least of them, 64 rows), one workgroup of 512 per row of a block,
+// and the tiles' 32-bit offsets.
 bool too_large(int64_t rows, int64_t V, int64_t ld_h, int64_t ld_w) {
-    return !grid_fits((rows + LmCfg::BM - 1) / LmCfg::BM * vocab_tiles(V), LmCfg::THREADS) ||
+    return !grid_fits((rows + X64::BM - 1) / X64::BM * column_tiles(V), X64::THREADS) ||
            !grid_fits(rows, 512) || ld_h > kMaxLd || ld_w > kMaxLd;
 }
+// the tile's rows of W and, slices past its last included, a run of panels (d <= kMaxLd)
+static_assert(rows_bytes(kTileN, kMaxLd, kMaxLd) < int64_t(1) << 31 &&
+                  (kMaxLd / kSliceK + 4) * kPanel < int64_t(1) << 31,
+              "32-bit offsets");
 
 }  // namespace
 
