@@ -593,8 +593,8 @@ typedef struct {
  * infinite logits show as NaN in the row's loss (and gradient).
  * Errors: INVALID_ARG for a null pointer, sizes or alignments that
  * dart_lmhead_tok_stats refuses, a value outside its range in config, or a
- * workspace that is too small; UNSUPPORTED when ceil(T/256) * ceil(V/256)
- * or T exceeds 8,388,607 or ld_h or ld_w 2^22; HIP when a launch fails. */
+ * workspace that is too small; UNSUPPORTED when ceil(T/64) * ceil(V/128) exceeds
+ * 16,777,215, T 8,388,607 or ld_h or ld_w 2^22; HIP when a launch fails. */
 dart_status_t dart_lmhead_xent_fwd(const void* hidden, int64_t T, int64_t d, int64_t ld_h,
                                    const void* weight, int64_t V, int64_t ld_w,
                                    const int32_t* target, const dart_xent_config_t* config,
@@ -634,9 +634,10 @@ dart_status_t dart_lmhead_xent_fwd_bwd(const void* hidden, int64_t T, int64_t d,
 
 /* Bytes of workspace of the two calls (0 for arguments outside
  * [1, INT32_MAX]). The second is chunk_rows * ceil8(V) * 2 for the
- * exponentials, chunk_rows * ceil(V/256) * 32 for partial sums, V * d * 4 where
- * chunk_rows < T, T * (2 d + 8) for the labelled rows, and at most
- * 64 MiB for dhidden's sum in parts where T and d are multiples of 256. Host only. */
+ * exponentials, chunk_rows * ceil(V/128) * 20 for partial sums, V * d * 4 where
+ * chunk_rows < T, T * (4 d + 8) for the labelled rows (padded to whole panels of 32 rows and 64
+ * columns once), and at most 64 MiB for dhidden's sum in parts where T and d are multiples of
+ * 256. Host only. */
 size_t dart_lmhead_xent_fwd_workspace_bytes(int64_t T, int64_t d, int64_t V);
 size_t dart_lmhead_xent_workspace_bytes(int64_t T, int64_t d, int64_t V, int64_t chunk_rows);
 
@@ -690,7 +691,7 @@ dart_status_t dart_mxfp4_dequantize(const void* q, int64_t R, int64_t K, dart_dt
  * The order of a sum, so its last bits, may differ between up to 32 rows of A and more.
  * Errors: INVALID_ARG for a null or misaligned pointer, a size outside
  * [1, INT32_MAX], ld_out < N or an unknown dtype; UNSUPPORTED when
- * ceil(M/256) * ceil(N/128) or ceil(N/32) exceeds 16,777,215 or K 16,777,216; HIP when a
+ * ceil(M/64) * ceil(N/128) or ceil(N/32) exceeds 16,777,215 or K 16,777,216; HIP when a
  * launch fails. */
 dart_status_t dart_mxfp4_matmul(const void* a, int64_t M, const void* b, int64_t N, int64_t K,
                                 dart_dtype_t dtype, void* out, int64_t ld_out, hipStream_t stream);
@@ -704,7 +705,7 @@ dart_status_t dart_mxfp4_matmul(const void* a, int64_t M, const void* b, int64_t
  *              (T * ceil(V/128) * 16 + T * 4), 16-byte aligned, owned by the
  *              caller; contents on entry do not matter.
  * Errors: INVALID_ARG as dart_lmhead_tok_stats_ex and for a null or misaligned
- * quantised matrix; UNSUPPORTED when ceil(T/256) * ceil(V/128)
+ * quantised matrix; UNSUPPORTED when ceil(T/64) * ceil(V/128)
  * or T exceeds 16,777,215 or d 16,777,216; HIP when a launch fails. */
 dart_status_t dart_lmhead_mxfp4_tok_stats(const void* hidden, int64_t T, const void* weight,
                                           int64_t V, int64_t d, const int32_t* target,

@@ -686,4 +686,23 @@ void with_tile(int bm, int64_t rows, int64_t V, F&& f) {
         f(LmCfg{});
 }
 
+// Tiles of 64, 128 or 256 rows x 128 columns, of which two run on a compute unit: the height
+// that forms rows x (128 column_tiles) fastest. A tile alone on its unit takes `alone`, with a
+// second one there `second` times that; where many wait, a unit finishes one every `each` (any
+// unit of time, and the same ratios at every depth measured).
+[[maybe_unused]] inline int fastest_height(int64_t rows, int64_t column_tiles,
+                                           const double (&alone)[3], const double (&each)[3],
+                                           double second) {
+    int best = 0;
+    double least = 0;
+    for (int k = 0; k < 3; ++k) {
+        const int bm = 64 << k;
+        const double per_unit = (double)((rows + bm - 1) / bm) * (double)column_tiles / kUnits;
+        const double cost = fmax(per_unit > 1 ? second * alone[k] : alone[k],
+                                 each[k] * (per_unit + 0.4));
+        if (best == 0 || cost < least) best = bm, least = cost;
+    }
+    return best;
+}
+
 }  // namespace
