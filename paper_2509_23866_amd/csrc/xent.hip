@@ -4,12 +4,12 @@
 // For the rows t whose target y_t lies in [0, V), with z = h W^T and lse_t = log sum_v e^z_tv:
 //   l_t   = (1 - eps) (lse_t - z_ty) + eps (lse_t - mean_v z_tv) + lambda lse_t^2
 //   dl/dz = (1 + 2 lambda lse_t) p_tv - (1 - eps) [v = y_t] - eps / V
-// and 0 for the others. Forward alone: the tile of lmhead_stats_kernel reduced to (max,
-// normaliser, sum) per row and 256 columns, merged per row. With the gradient, rows are
+// and 0 for the others. Forward alone: z is formed tile by tile, each row's columns of a tile
+// reduced to (largest, normaliser, sum), and these merged per row. With the gradient, rows are
 // taken a block at a time, and the product z is formed once:
-//   xent_tile_kernel  forms z tile by tile on the matrix cores, reduces each row's 256
-//                     columns to a triple, and keeps e = 2^15 e^(z - m) of them in fp16, m the
-//                     largest of 64 columns;
+//   xent_tile_kernel  forms z tile by tile on the matrix cores, reduces each row's 64-column
+//                     units to (m = the largest, the normaliser) and the sum of z, and keeps
+//                     e = 2^15 e^(z - m) in fp16;
 //   xent_rows_kernel  merges a row's triples to lse, and turns its e in place into the
 //                     bf16 dz / (1 - eps), from which no logit is needed;
 //   the GEMMs of the LM head's backward (dh = dz W, dW = dz^T h), times (1 - eps) / N.
@@ -48,7 +48,9 @@ __device__ __forceinline__ u32x2 pack_half4(float a, float b, float c, float d) 
 // MFMAs take them (below) and go from memory (L2) to registers; W's rows go through an LDS ring of NS
 // slices, from which the waves share them. With both operands in the LDS, as in gemm_tile, the
 // LDS is the limit; and two such workgroups fit a compute unit, so that one multiplies while the
-// other is in its epilogue. TILETIMES
+// other is in its epilogue. T = 4096, V = 152064, d = 3584: 3.40 ms with the exponentials kept and
+// 3.30 without (1.35 PFLOP/s; a library product of the size reaches 1.47 and stores its logits), where
+// gemm_tile with the same epilogues took 3.50 and 3.44; 12 rows of V = 4864, d = 2328: 19 us to 28.
 constexpr int kTileN = 128, kSliceK = 64;
 constexpr uint32_t kPanel = 4096;  // bytes
 template <int BM_, int WM_, int WN_, int NS_>
@@ -389,18 +391,20 @@ __device__ __forceinline__ RowSums joined(const RowSums& a, const RowSums& b) {
 // One workgroup of THREADS per row r of the block (of its first *n_rows - base): merges the
 // row's triples (lane-strided in index order, then a butterfly, then the waves in order),
 // adds the target logit last as lmhead_merge_kernel does, and writes the row's loss to
-// tok_loss[map[r]]. With KEEP the row of e becomes dz / (1 - eps) in bf16, in place.
+// tok_loss[map[r]]. With KEEP the row of e becomes dz / (1 - eps) in bf16, in place; where there
+// are few rows by segs workgroups, which all merge the row and then take a segment of it each.
 template <int THREADS, bool KEEP>
 __global__ void __launch_bounds__(THREADS)
 xent_rows_kernel(const float4* __restrict__ part, const float* __restrict__ z_sum,
                  const float* __restrict__ z_y, int64_t nvt, int64_t V,
                  const int32_t* __restrict__ target, const int32_t* __restrict__ map,
                  XentTerms terms, uint16_t* __restrict__ e, int64_t ld_e,
-                 float* __restrict__ tok_loss, const int32_t* __restrict__ n_rows, int64_t base) {
+                 float* __restrict__ tok_loss, const int32_t* __restrict__ n_rows, int64_t base,
+                 int64_t segs) {
     constexpr int WAVES = THREADS / 64;
     __shared__ RowSums waves[WAVES];
     const int tid = threadIdx.x, lane = tid & 63;
-    const int64_t r = blockIdx.x;
+    const int64_t r = blockIdx.x / segs, seg = blockIdx.x % segs;
     // (the row's own values all at once: they exist also past the labelled rows)
     const int32_t y = target[r], row_to = map[r];
     const float zy = z_y[r];
@@ -432,7 +436,7 @@ xent_rows_kernel(const float4* __restrict__ part, const float* __restrict__ z_su
     const float sx = x.s != 0.f ? x.s * expf(x.m - M) : 0.f, ey = expf(zy - M);
     const float ln_s = logf(sx + ey), lse = M + ln_s;
     const float logp = sx < ey ? -log1pf(sx / ey) : (zy - M) - ln_s;
-    if (tid == 0) {
+    if (tid == 0 && seg == 0) {
         const double l = (double)lse;
         double loss = -(double)logp * (1.0 - (double)terms.eps) + (double)terms.lambda * l * l;
         if (terms.eps > 0.f) loss += (double)terms.eps * (l - x.z / (double)V);
@@ -446,7 +450,8 @@ xent_rows_kernel(const float4* __restrict__ part, const float* __restrict__ z_su
             (expm1f(logp) + terms.eps + 2.f * terms.lambda * lse * expf(logp)) * keep - flat;
         typedef _Float16 h8 __attribute__((ext_vector_type(8)));
         const float* units = reinterpret_cast<const float*>(part + r * nvt);  // (m, s) of each
-        for (int64_t c = tid; c < chunks; c += THREADS) {
+        const int64_t each = (chunks + segs - 1) / segs, end = min(chunks, (seg + 1) * each);
+        for (int64_t c = seg * each + tid; c < end; c += THREADS) {
             const h8 q = __builtin_bit_cast(h8, row[c]);
             // the maximum of the chunk's unit
             const float m = units[c / (kStatsUnit / 8) * 2];
@@ -513,8 +518,9 @@ __device__ __forceinline__ void clear_row(int64_t t, int64_t d, float* __restric
 
 // One workgroup per row t: finds the row's place among the labelled ones by counting the labels
 // before it, and places or clears it; the first workgroup counts them all. For few rows
-// (kFewRows): 3 us at T = 48, 7 at 1000 and 19 at 4096, where the two kernels below take 8,
-// 12 and 20.
+// (kFewRows): 3.2 us at T = 48, 4.6 at 1000 and 8.6 at 4096 (d = 512; half the rows labelled),
+// where the two kernels below take 5.0, 5.8 and 9.7 and are a launch more, about 5 us where the
+// launches bound the call; d = 3584: 4.0, 7.4 and 15.0 to 6.7, 9.3 and 19.3.
 constexpr int kPrepareThreads = 256;
 constexpr int64_t kFewRows = 4096;
 __global__ void __launch_bounds__(kPrepareThreads)
@@ -669,16 +675,17 @@ int64_t ceil8(int64_t x) { return (x + 7) / 8 * 8; }
 // Parts of a block's dh sum over the vocabulary, as in the LM head's backward: dh's few tiles have
 // long sums, and the launch waits for them while they fill only some of the units. At most as
 // many as give every unit a part; none shorter than four slices of 64; and, as a slice takes
-// kSliceUs where few tiles run and a part is written and read once more, no more than make
-// slices * kSliceUs / n + n * rows * d * 8 bytes at 4 TB/s least. (48 rows of V = 4000, d = 512:
-// the products 66 us in one part, 15 in 7, PARTSUS in 15.)
-constexpr double kSliceUs = 0.75;
+// kSliceUs where few tiles run, and a part is written and read once more (rows * d * 8 bytes at 4
+// TB/s) and waited for (kPartUs), the n that makes slices * kSliceUs / n + n * part least. (48
+// rows of V = 4000, d = 512: the products 66 us in one part, 15 in 7, 12 in 15.)
+constexpr double kSliceUs = 0.75, kPartUs = 0.1;
 int64_t dh_parts(int64_t rows, int64_t d, int64_t V) {
     const int64_t tiles =
         ((rows + LmCfg::BM - 1) / LmCfg::BM) * ((d + LmCfg::BN - 1) / LmCfg::BN);
     const int64_t by_units = kUnits / tiles, by_k = V / (LmCfg::BK * 4);
-    const double slices = (double)V / LmCfg::BK, add_us = (double)rows * (double)d * 8 / 4e6;
-    const int64_t best = (int64_t)sqrt(slices * kSliceUs / add_us);
+    const double slices = (double)V / LmCfg::BK;
+    const double part_us = (double)rows * (double)d * 8 / 4e6 + kPartUs;
+    const int64_t best = (int64_t)sqrt(slices * kSliceUs / part_us);
     const int64_t n = by_units < by_k ? by_units : by_k;
     return n < best ? (n > 1 ? n : 1) : (best > 1 ? best : 1);
 }
@@ -755,7 +762,7 @@ void with_xent_cfg(int64_t rows, int64_t V, F&& f) {
 }
 
 // f(threads of a row's workgroup): about 16 vectors of eight columns each, which take turns with
-// the row's other latencies. 1220 rows of V = 1088: 16 us with 512, ROWSUS with 64.
+// the row's other latencies. 1220 rows of V = 1088: 16 us with 512, 7.6 with 64.
 template <class F>
 void with_row_threads(int64_t V, F&& f) {
     if (V <= 2048)
@@ -766,6 +773,14 @@ void with_row_threads(int64_t V, F&& f) {
         f(std::integral_constant<int, 256>{});
     else
         f(std::integral_constant<int, 512>{});
+}
+
+// Workgroups that share a row of e: as many as there is room for beside the other rows, each with
+// two rounds of its threads at least. 36 rows of V = 62036: 15 us by one each, 12 by 7.
+int64_t row_segments(int64_t rows, int64_t V, int threads) {
+    const int64_t room = 1024 / rows, most = (V + 7) / 8 / (2 * threads);
+    const int64_t n = room < most ? room : most;
+    return n > 1 ? n : 1;
 }
 
 // The whole call; without grads the loss alone.
@@ -834,14 +849,16 @@ dart_status_t run_xent(const uint16_t* h, int64_t T, int64_t d, int64_t ld_h, co
         if (!grads) {
             hipLaunchKernelGGL((xent_rows_kernel<64, false>), dim3((unsigned)rows), dim3(64), 0,
                                stream, part, z_sum, z_y, nvt, V, target_c + r0, map + r0, terms, e, ld_e,
-                               tok_loss, count, r0);
+                               tok_loss, count, r0, int64_t(1));
             continue;
         }
         with_row_threads(V, [&](auto threads) {
             constexpr int N = decltype(threads)::value;
-            hipLaunchKernelGGL((xent_rows_kernel<N, true>), dim3((unsigned)rows), dim3(N), 0, stream,
+            const int64_t segs = row_segments(rows, V, N);
+            hipLaunchKernelGGL((xent_rows_kernel<N, true>), dim3((unsigned)(rows * segs)), dim3(N), 0,
+                               stream,
                                part, z_sum, z_y, nvt, V, target_c + r0, map + r0, terms, e, ld_e, tok_loss,
-                               count, r0);
+                               count, r0, segs);
         });
         const dart_status_t st = lmhead::launch_bwd_gemms(
             e, ld_e, rows, V, w, ld_w, hr, d, d, parts && dh.p ? Grad{parts, d, false} : dh, false,
