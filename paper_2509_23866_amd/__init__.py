@@ -1177,10 +1177,26 @@ def dart_mxfp4_dequantize(q, dtype=None, out=None, stream=None):
     return out
 
 
-def _as_mxfp4(name, x, stream):
+def _rows_against(name, x, weight):
+    """The rows of ``x``, an Mxfp4 or a float32 or bfloat16 matrix that fits the Mxfp4 ``weight``."""
+    dev = weight.data.device
+    if isinstance(x, Mxfp4):
+        _check_mxfp4(name, x, dev)
+        shape = (x.rows, x.cols)
+    else:
+        if str(getattr(x, "dtype", None)) not in _FLOATS:
+            raise TypeError(f"{name} must be an Mxfp4 or a float32 or bfloat16 tensor")
+        if x.device != dev:
+            raise ValueError(f"{name} must be on {dev}")
+        shape = tuple(x.shape)
+    if len(shape) != 2 or shape[1] != weight.cols:
+        raise ValueError(f"{name} must be a matrix of the weight's inner size, {weight.cols}")
+    return shape[0]
+
+
+def _as_mxfp4(x, stream):
     """``x`` itself where it is an Mxfp4, else (a float32 or bfloat16 matrix) quantised."""
     if isinstance(x, Mxfp4):
-        _check_mxfp4(name, x)
         return x
     q = dart_mxfp4_quantize(x, stream=stream)
     _used_on(stream, q.data)
@@ -1201,11 +1217,9 @@ def dart_mxfp4_matmul(a, b, dtype=None, out=None, stream=None):
     if str(dtype) not in _FLOATS:
         raise TypeError("dtype must be float32 or bfloat16")
     dev = b.data.device
-    cols = a.cols if isinstance(a, Mxfp4) else a.shape[-1]
-    if cols != b.cols or (a.data if isinstance(a, Mxfp4) else a).device != dev:
-        raise ValueError("a and b must have the same inner size and be on one GPU")
-    a = _as_mxfp4("a", a, stream)
-    out = _out_matrix("out", out, (a.rows, b.rows), dtype, dev)
+    rows = _rows_against("a", a, b)
+    out = _out_matrix("out", out, (rows, b.rows), dtype, dev)
+    a = _as_mxfp4(a, stream)
     _enqueue("dart_mxfp4_matmul", dev, stream, a.data.data_ptr(), a.rows, b.data.data_ptr(), b.rows,
              b.cols, _FLOATS[str(dtype)], out.data_ptr(), _ld(out))
     return out
@@ -1226,10 +1240,7 @@ def dart_lmhead_mxfp4_tok_stats(hidden, weight, target, inv_temp=1.0, logp=None,
     torch = _torch()
     _check_mxfp4("weight", weight)
     dev = weight.data.device
-    cols = hidden.cols if isinstance(hidden, Mxfp4) else hidden.shape[-1]
-    if cols != weight.cols or (hidden.data if isinstance(hidden, Mxfp4) else hidden).device != dev:
-        raise ValueError("hidden and weight must have the same inner size d and be on one GPU")
-    T, V = hidden.rows if isinstance(hidden, Mxfp4) else hidden.shape[0], weight.rows
+    T, V = _rows_against("hidden", hidden, weight), weight.rows
     _check_vec("target", target, torch.int32, T, dev)
     logp = torch.empty(T, dtype=torch.float32, device=dev) if logp is None else logp
     entropy = torch.empty(T, dtype=torch.float32, device=dev) if entropy is None else entropy
@@ -1237,7 +1248,7 @@ def dart_lmhead_mxfp4_tok_stats(hidden, weight, target, inv_temp=1.0, logp=None,
     for n, v in (("logp", logp), ("entropy", entropy), ("lse", lse)):
         _check_vec(n, v, torch.float32, T, dev)
     workspace = _byte_workspace(workspace, dart_lmhead_mxfp4_stats_workspace_bytes(T, V), dev, stream)
-    hidden = _as_mxfp4("hidden", hidden, stream)
+    hidden = _as_mxfp4(hidden, stream)
     _enqueue("dart_lmhead_mxfp4_tok_stats", dev, stream, hidden.data.data_ptr(), T,
              weight.data.data_ptr(), V, weight.cols, target.data_ptr(), float(inv_temp), logp.data_ptr(), entropy.data_ptr(),
              lse.data_ptr(), workspace.data_ptr(), workspace.numel())

@@ -374,8 +374,11 @@ def test_refusals_with_tensors():
         dart.dart_mxfp4_dequantize(q._replace(data=q.data[1:]))
     with pytest.raises(ValueError):
         dart.dart_mxfp4_matmul(x[:, :32].contiguous(), q)
-    with pytest.raises(TypeError):
-        dart.dart_mxfp4_matmul(q, x)
+    for bad in ((q, x), ("x", q), (None, q)):
+        with pytest.raises(TypeError):
+            dart.dart_mxfp4_matmul(*bad)
+    with pytest.raises(ValueError):
+        dart.dart_mxfp4_matmul(x.cpu(), q)
     with pytest.raises(TypeError):
         dart.dart_mxfp4_matmul(q, q, dtype=torch.float16)
     with pytest.raises(ValueError):
