@@ -33,7 +33,7 @@ that lmhead_backward_plan picks for a 512 MiB workspace.
 
 import torch
 
-from . import (DART_LMHEAD_BF16_GRADS, dart_grad_scale, dart_lmhead_backward_ex,
+from . import (DART_LMHEAD_BF16_GRADS, _nat, dart_grad_scale, dart_lmhead_backward_ex,
                dart_lmhead_tok_stats_ex, dart_lmhead_xent_fwd, dart_lmhead_xent_fwd_bwd,
                dart_select_tis_loss_fwd, dart_tis_grad, dart_tok_stats, lmhead_backward_plan)
 
@@ -158,40 +158,28 @@ class DartLmHeadXent(torch.autograd.Function):
         return tuple(None if g is None else dart_grad_scale(g, factor) for g in grads) + (None,) * 3
 
 
-_LEAF_STREAM = "dart_lmhead_xent_loss stream"
-
-
 def _refuse_mixed_capture(leaves):
     """torch's engine ends a backward pass by having the stream on which a leaf's gradient
     accumulator was made wait for it. That node lives as long as any graph of the leaf: under HIP
-    graph capture, one that an eager loss made on another stream would pull that stream into the
-    capture, which ends the process. So a loss leaves its stream with the node (_mark_leaves), and
-    under capture a node with another's is refused."""
+    graph capture, one that an eager computation made on another stream would pull that stream into
+    the capture, which ends the process."""
     for leaf in leaves:
-        made_on = torch.autograd.graph.get_gradient_edge(leaf).node.metadata.get(_LEAF_STREAM)
-        if made_on not in (None, torch.cuda.current_stream(leaf.device).cuda_stream):
-            raise RuntimeError("a loss of this leaf from another stream is still alive: release it "
+        made_on = _nat(required=True).accumulator_stream(leaf)
+        if made_on not in (None, torch.cuda.current_stream(leaf.device).stream_id):
+            raise RuntimeError("a graph of this leaf that was made on another stream is still alive: "
+                               "release it (the loss, or whatever else was computed from the leaf) "
                                "before capturing a backward pass of the leaf")
-
-
-def _mark_leaves(leaves):
-    """Once the loss's graph holds the leaves' accumulators."""
-    for leaf in leaves:
-        torch.autograd.graph.get_gradient_edge(leaf).node.metadata.setdefault(
-            _LEAF_STREAM, torch.cuda.current_stream(leaf.device).cuda_stream)
 
 
 def dart_lmhead_xent_loss(hidden, weight, target, label_smoothing=0.0, z_loss=0.0,
                           reduction="mean", chunk_rows=None):
     """Differentiable cross entropy of the LM head's inputs (see the module docstring);
     arguments as for dart_lmhead_xent_fwd_bwd. Rows with a negative target do not count. Under
-    HIP graph capture no eager loss of the same leaves may be alive (a RuntimeError where it is one
-    of these; for others' graphs torch does not say)."""
+    HIP graph capture no graph of the same leaves made on another stream, such as an eager loss, may
+    be alive (a RuntimeError)."""
     want = tuple(torch.is_grad_enabled() and t.requires_grad for t in (hidden, weight))
     leaves = [t for t, wanted in zip((hidden, weight), want) if wanted and t.is_leaf and t.is_cuda]
     if leaves and torch.cuda.is_current_stream_capturing():
         _refuse_mixed_capture(leaves)
-    loss = DartLmHeadXent.apply(hidden, weight, target,
+    return DartLmHeadXent.apply(hidden, weight, target,
                                 (float(label_smoothing), float(z_loss), reduction, chunk_rows), want)
-    _mark_leaves(leaves)
-    return loss

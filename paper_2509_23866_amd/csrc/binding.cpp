@@ -17,7 +17,9 @@
 #include <dlfcn.h>
 #include <torch/csrc/Dtype.h>
 #include <torch/csrc/Exceptions.h>
+#include <torch/csrc/autograd/function.h>
 #include <torch/csrc/autograd/python_variable.h>
+#include <torch/csrc/autograd/variable.h>
 
 #include "dart.h"
 
@@ -616,6 +618,17 @@ NATIVE(lmhead_mxfp4_tok_stats, 4)
     return st == DART_OK ? tuple(o.logp, o.entropy, o.lse) : failed(place, st);
 NATIVE_END
 
+// The id of the stream on which the tensor's gradient accumulator was made; None where it has
+// none, no graph of the tensor being alive.
+NATIVE(accumulator_stream, 1)
+    if (!THPVariable_Check(a[0])) Py_RETURN_NONE;
+    const auto node = torch::autograd::impl::try_get_grad_accumulator(THPVariable_Unpack(a[0]));
+    if (!node) Py_RETURN_NONE;
+    const std::optional<c10::Stream> s = node->stream();
+    if (!s) Py_RETURN_NONE;
+    return PyLong_FromLongLong(s->id());
+NATIVE_END
+
 // open(path): the C functions of the library at path.
 PyObject* open_lib(PyObject*, PyObject* arg) {
     const char* path = PyUnicode_AsUTF8(arg);
@@ -638,7 +651,7 @@ PyMethodDef methods[] = {
     ENTRY(grpo_advantage), ENTRY(step_select_groups), ENTRY(tis_loss_fwd_ex),
     ENTRY(lmhead_tok_stats), ENTRY(lmhead_xent_fwd), ENTRY(lmhead_xent_fwd_bwd),
     ENTRY(mxfp4_quantize), ENTRY(mxfp4_dequantize), ENTRY(mxfp4_matmul),
-    ENTRY(lmhead_mxfp4_tok_stats), {"open", open_lib, METH_O, nullptr}, {nullptr, nullptr, 0, nullptr}};
+    ENTRY(lmhead_mxfp4_tok_stats), ENTRY(accumulator_stream), {"open", open_lib, METH_O, nullptr}, {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module_def = {PyModuleDef_HEAD_INIT, "_native", nullptr, -1, methods,
                           nullptr, nullptr, nullptr, nullptr};
 

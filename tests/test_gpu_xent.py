@@ -392,6 +392,41 @@ def test_captured_backward():
             assert torch.equal(a, b) and torch.equal(a, c)
 
 
+def test_capture_is_refused_beside_any_graph_of_a_leaf():
+    """Whatever made the leaf's accumulator on another stream; one made by the same capture is
+    no reason."""
+    import torch
+
+    from paper_2509_23866_amd.autograd import dart_lmhead_xent_loss
+
+    h, w, y = _problem(40, 64, 300)
+    hd, wd, yd = _dev(h), _dev(w).requires_grad_(), _ids(y)
+    alive = (wd.float() ** 2).sum()
+    refused = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(refused):
+        kept = yd + 1
+        with pytest.raises(RuntimeError, match="still alive"):
+            dart_lmhead_xent_loss(hd, wd, yd)
+    refused.replay()
+    torch.cuda.synchronize()
+    assert torch.equal(kept, yd + 1)
+    del alive
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        first = dart_lmhead_xent_loss(hd, wd, yd)
+        second = dart_lmhead_xent_loss(hd, wd, yd, 0.1)
+        got = (first.detach(), second.detach(), torch.autograd.grad(first + second, wd)[0])
+    del first, second
+    for _ in range(3):
+        graph.replay()
+        torch.cuda.synchronize()
+        a, b = dart_lmhead_xent_loss(hd, wd, yd), dart_lmhead_xent_loss(hd, wd, yd, 0.1)
+        want = (a.detach(), b.detach(), torch.autograd.grad(a + b, wd)[0])
+        del a, b
+        for x, z in zip(got, want):
+            assert torch.equal(x, z)
+
+
 def test_checks_report_ids_past_the_vocabulary(monkeypatch):
     dart = _dart()
     h, w, y = _problem(20, 16, 50)
