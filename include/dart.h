@@ -9,6 +9,8 @@
  *   2. per-step mean entropy and the high-entropy step mask     dart_step_select
  *   3. the truncated-importance-sampling-weighted clipped
  *      policy-gradient loss and its gradient w.r.t. the logits  dart_tis_loss_fwd_bwd
+ * Further sections take the same from the LM head's inputs, its supervised loss
+ * (dart_lmhead_xent_fwd_bwd) and the head in four bits (dart_mxfp4_*).
  *
  * Conventions shared by every call
  * --------------------------------

@@ -1,7 +1,7 @@
 """Python binding of libdart (the C ABI declared in include/dart.h).
 
-Argument marshalling only: every step of the path runs in the HIP kernels of
-``csrc/dart.hip``. torch supplies device memory and the stream. The library must
+Argument marshalling only: every step of the path runs in the HIP kernels under
+``csrc/``. torch supplies device memory and the stream. The library must
 be built (``__graft_entry__.build()``); if it is missing, importing a function
 raises — there is no CPU fallback. Calls whose arguments are plain tensors, with
 the outputs left to the call and on the current stream, are marshalled natively
@@ -13,7 +13,11 @@ Functions carry the C names: ``dart_tok_stats``, ``dart_step_select``,
 ``dart_tis_grad``), the ``_ex`` variants (inverse temperature, the KL term,
 aggregation and ratio level, zero-row skipping), ``dart_tis_loss_workspace_bytes``,
 ``dart_kept_steps`` and ``dart_status_string``. ``policy_update`` chains the
-device calls.
+device calls. From the LM head's inputs: ``dart_lmhead_tok_stats`` and
+``dart_lmhead_backward``; its supervised loss, ``dart_lmhead_xent_fwd`` and, with
+the gradients, ``dart_lmhead_xent_fwd_bwd``; and the head in four bits,
+``dart_mxfp4_quantize`` (an ``Mxfp4``), ``dart_mxfp4_dequantize``,
+``dart_mxfp4_matmul`` and ``dart_lmhead_mxfp4_tok_stats``.
 """
 
 from __future__ import annotations
