@@ -686,6 +686,21 @@ void with_tile(int bm, int64_t rows, int64_t V, F&& f) {
         f(LmCfg{});
 }
 
+// The part of a tile of configuration C that is left where its wave's first row blocks have all
+// of the matrix's rows: one row block a wave, the first C::RS rows.
+template <class C>
+struct FirstRows : C {
+    static constexpr int BM = C::RS, TM = 1;
+};
+
+// f(C, or FirstRows<C> where that has the last of the M rows) for a tile whose first row is m0.
+template <class C, class F>
+__device__ __forceinline__ void with_rows_of(int64_t M, int64_t m0, F&& f) {
+    if constexpr (C::TM > 1)
+        if (M - m0 <= C::RS) return f(FirstRows<C>{});
+    f(C{});
+}
+
 // Tiles of 64, 128 or 256 rows x 128 columns, of which two run on a compute unit: the height
 // that forms rows x (128 column_tiles) fastest. A tile alone on its unit takes `alone`, with a
 // second one there `second` times that; where many wait, a unit finishes one every `each` (any
@@ -697,7 +712,10 @@ void with_tile(int bm, int64_t rows, int64_t V, F&& f) {
     double least = 0;
     for (int k = 0; k < 3; ++k) {
         const int bm = 64 << k;
-        const double per_unit = (double)((rows + bm - 1) / bm) * (double)column_tiles / kUnits;
+        // the last height of 256 takes as long as one of 128 where that is enough (FirstRows)
+        const int64_t tail = rows % bm;
+        const double last = tail == 0 ? 0 : k == 2 && tail <= 128 ? each[1] / each[2] : 1;
+        const double per_unit = ((double)(rows / bm) + last) * (double)column_tiles / kUnits;
         const double cost = fmax(per_unit > 1 ? second * alone[k] : alone[k],
                                  each[k] * (per_unit + 0.4));
         if (best == 0 || cost < least) best = bm, least = cost;

@@ -487,23 +487,25 @@ __device__ __forceinline__ void store_tile(f32x16 (&acc)[C::TM][C::TN], int64_t 
         }
 }
 
-// f(LDS, first row, column tile) for this workgroup's tile of M rows x nnt column tiles.
+// f(configuration, LDS, first row, column tile) for this workgroup's tile of M rows x nnt column
+// tiles.
 template <class C, class F>
 __device__ __forceinline__ void with_mxfp4_tile(int64_t M, int64_t nnt, F&& f) {
     __shared__ typename C::Smem sm;
     int64_t mt, nt;
     tile_of_block((M + C::BM - 1) / C::BM, nnt, mt, nt);
-    f(sm, mt * C::BM, nt);
+    with_rows_of<C>(M, mt * C::BM, [&](auto c) { f(c, sm, mt * C::BM, nt); });
 }
 
 template <class C, class O>
 __global__ void __launch_bounds__(C::THREADS, 2)
 mxfp4_matmul_kernel(Mxfp4Pair x, int64_t M, int64_t N, int64_t nnt, O* __restrict__ out,
                     int64_t ld) {
-    with_mxfp4_tile<C>(M, nnt, [&](auto& sm, int64_t m0, int64_t nt) {
-        f32x16 acc[C::TM][C::TN];
-        mxfp4_tile<C>(x, m0, nt * C::BN, sm, acc);
-        store_tile<C, O>(acc, M, N, out, ld, sm, m0, nt * C::BN);
+    with_mxfp4_tile<C>(M, nnt, [&](auto c, auto& sm, int64_t m0, int64_t nt) {
+        using P = decltype(c);
+        f32x16 acc[P::TM][P::TN];
+        mxfp4_tile<P>(x, m0, nt * P::BN, sm, acc);
+        store_tile<P, O>(acc, M, N, out, ld, sm, m0, nt * P::BN);
     });
 }
 
@@ -511,9 +513,10 @@ template <class C>
 __global__ void __launch_bounds__(C::THREADS, 2)
 mxfp4_stats_kernel(Mxfp4Pair x, int64_t T, int64_t V, const int32_t* __restrict__ target,
                    float scale, int64_t nvt, float4* __restrict__ part, float* __restrict__ z_y) {
-    with_mxfp4_tile<C>(T, nvt, [&](auto& sm, int64_t m0, int64_t vt) {
-        stats_of_tile<C>(
-            [&](int64_t n0, f32x16(&acc)[C::TM][C::TN]) { mxfp4_tile<C>(x, m0, n0, sm, acc); }, T, V,
+    with_mxfp4_tile<C>(T, nvt, [&](auto c, auto& sm, int64_t m0, int64_t vt) {
+        using P = decltype(c);
+        stats_of_tile<P>(
+            [&](int64_t n0, f32x16(&acc)[P::TM][P::TN]) { mxfp4_tile<P>(x, m0, n0, sm, acc); }, T, V,
             target, scale, nvt, part, z_y, sm, m0, vt);
     });
 }

@@ -367,8 +367,10 @@ xent_tile_kernel(const uint8_t* __restrict__ h, int64_t M, const uint16_t* __res
     if ((int64_t)blockIdx.x >= nmt * nvt) return;
     int64_t mt, vt;
     tile_of_block(nmt, nvt, mt, vt);
-    xent_tile<C, KEEP>(h, M, w, V, ldw, d, target, sums != 0, nvt, part, z_sum, z_y, e, ld_e, sm,
-                       mt * C::BM, vt);
+    with_rows_of<C>(M, mt * C::BM, [&](auto c) {
+        xent_tile<decltype(c), KEEP>(h, M, w, V, ldw, d, target, sums != 0, nvt, part, z_sum, z_y, e,
+                                     ld_e, sm, mt * C::BM, vt);
+    });
 }
 
 // The objective's constants.
