@@ -97,12 +97,12 @@ struct Grad {
 // the sum. With dh_map row i of dh goes to row dh_map[i] of dh_out. With dyn_rows,
 // the block's rows are at most *dyn_rows - dyn_base (read on the device).
 // A null dh_out.p or dw_out.p leaves that product out; scale (device memory, may be
-// null) is a factor of both.
+// null) is a factor of both. small: in tiles of 128 x 128 in place of 256 x 256 (not with dh_acc).
 __attribute__((visibility("hidden"))) dart_status_t launch_bwd_gemms(
     const uint16_t* dz, int64_t ld_dz, int64_t rows, int64_t cols, const uint16_t* w, int64_t ld_w,
     const uint16_t* h, int64_t ld_h, int64_t d, const Grad& dh_out, bool dh_acc, int64_t ksplit,
     int64_t part_stride, const Grad& dw_out, bool dw_acc, hipStream_t stream, const int32_t* dh_map,
-    const int32_t* dyn_rows, int64_t dyn_base, const float* scale);
+    const int32_t* dyn_rows, int64_t dyn_base, const float* scale, bool small);
 
 // dst [rows, cols] in bf16 from fp32 rows of cols elements.
 __attribute__((visibility("hidden"))) void launch_to_bf16(const float* src, int64_t rows,

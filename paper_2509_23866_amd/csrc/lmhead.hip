@@ -425,6 +425,198 @@ __device__ __forceinline__ void gemm_tile_bwd(const uint16_t* __restrict__ A, in
 #endif
 }
 
+// The same for small tiles of four waves, of which three fit a compute unit, so that some multiply
+// while others begin or store: slices of 32 through a ring of three buffers, every wave its own
+// loads. Sums run over k in the same order. (128 x 256 in two a unit was the fastest of the three
+// in 6 of 110 sizes, by 3%.)
+using BwdSmall = Cfg<128, 128, 2, 2, 3, 32>;
+
+template <class C, bool A_KMAJ>
+__device__ __forceinline__ void gemm_tile_bwd_ring(const uint16_t* __restrict__ A, int64_t lda,
+                                                   const uint16_t* __restrict__ B, int64_t ldb,
+                                                   int64_t M, int64_t N, int64_t kbeg, int64_t K,
+                                                   int64_t m0, int64_t n0, typename C::Smem& sm,
+                                                   f32x16 (&acc)[C::TM][C::TN]) {
+#if defined(__HIP_DEVICE_COMPILE__)
+    static_assert(C::NS == 3 && C::WAVES == 4, "ring of three, four waves");
+    constexpr int BK = C::BK, CH = C::CH;
+    const int tid = threadIdx.x, lane = tid & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int wr = (wave / C::WN) * 32, wc = (wave % C::WN) * (C::BN / C::WN);
+#pragma unroll
+    for (int i = 0; i < C::TM; ++i)
+#pragma unroll
+        for (int j = 0; j < C::TN; ++j)
+#pragma unroll
+            for (int v = 0; v < 16; ++v) acc[i][j][v] = 0.f;
+    const int64_t nk = (K + BK - 1) / BK;
+    constexpr uint32_t kNowhere = 0x80000000u;  // past any resource here: less than 2^31 bytes
+
+    // Loads of a transposed operand, W elements wide: an instruction fills 512 / W rows, the
+    // wave's q-th the rows (q * 4 + wave) * (512 / W) and on (a lane's row modulo 4, and so
+    // its slot's chunk, is the same for every q).
+    constexpr int RPA = 512 / C::BM, RPB = 512 / C::BN;      // rows an instruction
+    constexpr int QA = A_KMAJ ? C::IA : BK / RPA / C::WAVES, QB = BK / RPB / C::WAVES;
+    static_assert(QB * RPB * C::WAVES == BK && C::WAVES * RPB % 4 == 0, "transposed rows per wave");
+    static_assert(A_KMAJ || (QA * RPA * C::WAVES == BK && C::WAVES * RPA % 4 == 0), "as above");
+    uint32_t va, qa;
+    if constexpr (A_KMAJ) {
+        const int r = wave * C::LROWS + lane / CH;
+        va = (uint32_t)((r * lda + (lane % CH ^ swz<CH>(r)) * 8) * 2);
+        qa = (uint32_t)(C::WAVES * C::LROWS * lda * 2);
+    } else {
+        const int k = wave * RPA + lane / (C::BM / 8);
+        va = (uint32_t)((k * lda + tr_slot(lane % (C::BM / 8), k) * 8) * 2);
+        qa = (uint32_t)(C::WAVES * RPA * lda * 2);
+    }
+    const int kb = wave * RPB + lane / (C::BN / 8);
+    const uint32_t vb = (uint32_t)((kb * ldb + tr_slot(lane % (C::BN / 8), kb) * 8) * 2);
+    const uint32_t qb = (uint32_t)(C::WAVES * RPB * ldb * 2);
+    const __amdgpu_buffer_rsrc_t rak =
+        tile_rsrc(A + m0 * lda, A_KMAJ ? (M - m0 < C::BM ? M - m0 : C::BM) * lda * 2 : 0);
+    // a transposed operand's slice: rows kt * BK .. K - 1 from column t0; none past the last
+    auto tr_rsrc = [&](const uint16_t* X, int64_t ld, int64_t t0, int64_t len, int64_t kt) {
+        const int64_t first = (kt < nk ? kt : 0) * BK * ld + t0;
+        const int64_t end = (K - 1) * ld + (len + 7) / 8 * 8;
+        return tile_rsrc(X + first, kt < nk ? (end - first) * 2 : 0);
+    };
+    auto issue = [&](int64_t kt, int buf) {
+        if constexpr (A_KMAJ) {
+            const uint32_t at = kt < nk ? (uint32_t)(kt * BK * 2) : 0u;
+#pragma unroll
+            for (uint32_t q = 0; q < QA; ++q)
+                __builtin_amdgcn_raw_ptr_buffer_load_lds(
+                    rak, lds_ptr(&sm.in.a[buf][0][0] + (q * C::WAVES + wave) * 512), 16,
+                    kt < nk ? va : kNowhere, kt < nk ? at + q * qa : 0u, 0, 0);
+        } else {
+            const __amdgpu_buffer_rsrc_t ra = tr_rsrc(A, lda, m0, M, kt);
+#pragma unroll
+            for (uint32_t q = 0; q < QA; ++q)
+                __builtin_amdgcn_raw_ptr_buffer_load_lds(
+                    ra, lds_ptr(&sm.in.a[buf][0][0] + (q * C::WAVES + wave) * 512), 16, va, q * qa,
+                    0, 0);
+        }
+        const __amdgpu_buffer_rsrc_t rb = tr_rsrc(B, ldb, n0, N, kt);
+#pragma unroll
+        for (uint32_t q = 0; q < QB; ++q)
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(
+                rb, lds_ptr(&sm.in.b[buf][0][0] + (q * C::WAVES + wave) * 512), 16, vb, q * qb, 0, 0);
+    };
+
+    // operand offsets in a slice, as in gemm_tile_bwd; opaque, so that buffer, k-step and half
+    // are the reads' immediates
+    const char* const lds0 = reinterpret_cast<const char*>(&sm);
+    const int kq = (lane >> 2) & 3, tr_row = 8 * (lane >> 5) + kq;
+    const int tr_delta = 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1);
+    auto tr_off = [&](int mb, int width) -> uint32_t {
+        const int slot = ((mb / 8) ^ (4 * kq)) | tr_delta;
+        return (uint32_t)(tr_row * width * 2 + slot * 16 + 8 * (lane & 1));
+    };
+    uint32_t rda[A_KMAJ ? C::KSTEPS : C::TM], rdb[C::TN];
+    if constexpr (A_KMAJ) {
+#pragma unroll
+        for (int ks = 0; ks < C::KSTEPS; ++ks) {
+            const int c = ks * 2 + (lane >> 5), r = wr + (lane & 31);
+            rda[ks] = (uint32_t)(r * BK + (c ^ swz<CH>(r)) * 8) * 2;
+            asm volatile("" : "+v"(rda[ks]));
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < C::TM; ++i) {
+            rda[i] = tr_off(wr + i * C::RS, C::BM);
+            asm volatile("" : "+v"(rda[i]));
+        }
+    }
+    const uint32_t b_at = (uint32_t)(reinterpret_cast<const char*>(&sm.in.b[0][0][0]) - lds0);
+#pragma unroll
+    for (int j = 0; j < C::TN; ++j) {
+        rdb[j] = b_at + tr_off(wc + j * 32, C::BN);
+        asm volatile("" : "+v"(rdb[j]));
+    }
+    auto tr_pair = [&](uint32_t at, int width) -> bf16x8 {
+        const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_ptr)(lds0 + at));
+        const s16x4 hi =
+            __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_ptr)(lds0 + at + 4 * width * 2));
+        typedef short s16x8 __attribute__((ext_vector_type(8)));
+        const s16x8 v = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
+        return __builtin_bit_cast(bf16x8, v);
+    };
+    bf16x8 af[2][C::TM], bfr[2][C::TN];
+    auto read_step = [&](auto bufc, int ks, int set) {
+        constexpr int buf = decltype(bufc)::value;
+#pragma unroll
+        for (int i = 0; i < C::TM; ++i) {
+            if constexpr (A_KMAJ)
+                af[set][i] = __builtin_bit_cast(
+                    bf16x8, *reinterpret_cast<const u32x4*>(lds0 + rda[ks] + buf * C::BM * BK * 2 +
+                                                            i * C::RS * BK * 2));
+            else
+                af[set][i] = tr_pair(rda[i] + buf * C::BM * BK * 2 + ks * 16 * C::BM * 2, C::BM);
+        }
+#pragma unroll
+        for (int j = 0; j < C::TN; ++j)
+            bfr[set][j] = tr_pair(rdb[j] + buf * C::BN * BK * 2 + ks * 16 * C::BN * 2, C::BN);
+    };
+    // k past K of a K-major A (also inside the chunk that straddles K) set to 0
+    auto zero_tail = [&](int64_t kt, int buf) {
+        const int kv = (int)(K - kt * BK);
+        uint16_t* a = &sm.in.a[buf][0][0];
+        for (int e = tid; e < BK * C::BM; e += C::THREADS) {
+            const int r = e / BK, kk = ((e % BK / 8) ^ swz<CH>(r)) * 8 + e % 8;
+            if (kk >= kv) a[e] = 0;
+        }
+    };
+    auto slice = [&](auto bufc, int64_t kt) {
+        constexpr int buf = decltype(bufc)::value;
+        wait_vmcnt<QA + QB>();  // the loads of slice kt + 1
+        lds_ring_barrier();
+        if (A_KMAJ && (K % BK) && kt == nk - 1) {
+            zero_tail(kt, buf);
+            lds_ring_barrier();
+        }
+        issue(kt + 2, (buf + 2) % 3);
+        __builtin_amdgcn_sched_barrier(0);
+        read_step(bufc, 0, 0);
+        __builtin_amdgcn_sched_barrier(0);
+        __builtin_amdgcn_s_setprio(1);
+#pragma unroll
+        for (int ks = 0; ks < C::KSTEPS; ++ks) {
+            if (ks + 1 < C::KSTEPS) read_step(bufc, ks + 1, (ks & 1) ^ 1);
+#pragma unroll
+            for (int i = 0; i < C::TM; ++i)
+#pragma unroll
+                for (int j = 0; j < C::TN; ++j)
+                    acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(bfr[ks & 1][j], af[ks & 1][i],
+                                                                        acc[i][j], 0, 0, 0);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        __builtin_amdgcn_s_setprio(0);
+        // the products stay in their slice
+#pragma unroll
+        for (int i = 0; i < C::TM; ++i)
+#pragma unroll
+            for (int j = 0; j < C::TN; ++j) asm volatile("" : "+v"(acc[i][j]));
+    };
+    int64_t kt = kbeg / BK;
+    if (kt < nk) {
+        issue(kt, 0);
+        issue(kt + 1, 1);
+        for (; kt + 2 < nk; kt += 3) {
+            slice(std::integral_constant<int, 0>{}, kt);
+            slice(std::integral_constant<int, 1>{}, kt + 1);
+            slice(std::integral_constant<int, 2>{}, kt + 2);
+        }
+        if (kt < nk) slice(std::integral_constant<int, 0>{}, kt);
+        if (kt + 1 < nk) slice(std::integral_constant<int, 1>{}, kt + 1);
+    }
+    wait_vmcnt<0>();  // the zeros of slices past the last are in LDS
+    __syncthreads();
+#else
+    (void)A, (void)lda, (void)B, (void)ldb, (void)M, (void)N, (void)kbeg, (void)K, (void)m0;
+    (void)n0, (void)sm, (void)acc;
+#endif
+}
+
 // One GEMM of the backward: C[M, N] (+)= A B with gemm_tile_bwd's operands,
 // written to out [M, ldc] (fp32, or bf16 bits rounded to nearest even); vec:
 // out 16-byte aligned and ldc a multiple of 16 bytes' worth of elements.
@@ -503,7 +695,10 @@ __device__ __forceinline__ void bwd_gemm_tile(const BwdGemm& g, int64_t b, typen
     const int64_t m0 = mt * C::BM, n0 = nt * C::BN;
     const float f = g.scale ? *g.scale : 1.f;  // here, where its latency is hidden
     f32x16 acc[C::TM][C::TN];
-    gemm_tile_bwd<C, A_KMAJ>(g.A, g.lda, g.B, g.ldb, M, N, kbeg, K, m0, n0, sm, acc);
+    if constexpr (C::WAVES == 4)
+        gemm_tile_bwd_ring<C, A_KMAJ>(g.A, g.lda, g.B, g.ldb, M, N, kbeg, K, m0, n0, sm, acc);
+    else
+        gemm_tile_bwd<C, A_KMAJ>(g.A, g.lda, g.B, g.ldb, M, N, kbeg, K, m0, n0, sm, acc);
     if (g.scale) {
 #pragma unroll
         for (int i = 0; i < C::TM; ++i)
@@ -588,7 +783,7 @@ __device__ __forceinline__ void bwd_gemm_tile(const BwdGemm& g, int64_t b, typen
 // with a short one, so dW's tiles fill the compute units that dh leaves
 // free, and both start from the dz block just written.
 template <class C, int DH_OUT, int DW_OUT>
-__global__ void __launch_bounds__(C::THREADS)
+__global__ void __launch_bounds__(C::THREADS, C::WAVES == 4 ? 3 : 1)
 lmhead_bwd_gemms_kernel(BwdGemm dh, BwdGemm dw, int64_t n_dh) {
     __shared__ typename C::Smem sm;
     const int64_t b = blockIdx.x;
@@ -933,14 +1128,14 @@ BackwardPlan plan_backward(int64_t T, int64_t d, int64_t V, int64_t chunk_rows,
 // The GEMM description of one backward output (out.p at the block's first
 // row); mode: kOutF32, kOutF32Acc or kOutBf16.
 BwdGemm make_bwd_gemm(const uint16_t* A, int64_t lda, const uint16_t* B, int64_t ldb, int64_t M,
-                      int64_t N, int64_t K, const Grad& out) {
+                      int64_t N, int64_t K, const Grad& out, int bm, int bn) {
     BwdGemm g;
     g.A = A, g.lda = lda, g.B = B, g.ldb = ldb, g.M = M, g.N = N, g.K = K;
     g.out = out.p, g.ldc = out.ld;
     const size_t esz = out.bf16 ? 2 : 4;
     g.vec = reinterpret_cast<uintptr_t>(out.p) % 16 == 0 && (out.ld * esz) % 16 == 0;
-    g.nmt = (M + LmCfg::BM - 1) / LmCfg::BM;
-    g.nnt = (N + LmCfg::BN - 1) / LmCfg::BN;
+    g.nmt = (M + bm - 1) / bm;
+    g.nnt = (N + bn - 1) / bn;
     g.dyn = nullptr, g.dyn_base = 0, g.dyn_m = g.dyn_k = false;
     g.map = nullptr, g.ksplit = 1, g.kper = K, g.part_stride = 0;
     g.scale = nullptr;
@@ -951,19 +1146,28 @@ int out_mode(const Grad& out, bool accumulate) {
     return out.bf16 ? kOutBf16 : accumulate ? kOutF32Acc : kOutF32;
 }
 
-template <int DH, int DW>
+template <class C, int DH, int DW>
 void launch_bwd_gemms_t(const BwdGemm& dh, const BwdGemm& dw, int64_t n_dh, int64_t blocks,
                         hipStream_t stream) {
-    hipLaunchKernelGGL((lmhead_bwd_gemms_kernel<LmCfg, DH, DW>), dim3((unsigned)blocks),
-                       dim3(LmCfg::THREADS), 0, stream, dh, dw, n_dh);
+    hipLaunchKernelGGL((lmhead_bwd_gemms_kernel<C, DH, DW>), dim3((unsigned)blocks),
+                       dim3(C::THREADS), 0, stream, dh, dw, n_dh);
 }
 
-template <int DH>
+template <class C, int DH>
 void launch_bwd_gemms_dw(int dw_mode, const BwdGemm& dh, const BwdGemm& dw, int64_t n_dh,
                          int64_t blocks, hipStream_t stream) {
-    if (dw_mode == kOutF32) launch_bwd_gemms_t<DH, kOutF32>(dh, dw, n_dh, blocks, stream);
-    else if (dw_mode == kOutF32Acc) launch_bwd_gemms_t<DH, kOutF32Acc>(dh, dw, n_dh, blocks, stream);
-    else launch_bwd_gemms_t<DH, kOutBf16>(dh, dw, n_dh, blocks, stream);
+    if (dw_mode == kOutF32) launch_bwd_gemms_t<C, DH, kOutF32>(dh, dw, n_dh, blocks, stream);
+    else if (dw_mode == kOutF32Acc) launch_bwd_gemms_t<C, DH, kOutF32Acc>(dh, dw, n_dh, blocks, stream);
+    else launch_bwd_gemms_t<C, DH, kOutBf16>(dh, dw, n_dh, blocks, stream);
+}
+
+template <class C>
+void launch_bwd_gemms_c(int dh_mode, int dw_mode, const BwdGemm& dh, const BwdGemm& dw, int64_t n_dh,
+                        int64_t blocks, hipStream_t stream) {
+    if (dh_mode == kOutF32) launch_bwd_gemms_dw<C, kOutF32>(dw_mode, dh, dw, n_dh, blocks, stream);
+    else if (dh_mode == kOutBf16) launch_bwd_gemms_dw<C, kOutBf16>(dw_mode, dh, dw, n_dh, blocks, stream);
+    else if constexpr (std::is_same<C, LmCfg>::value)
+        launch_bwd_gemms_dw<C, kOutF32Acc>(dw_mode, dh, dw, n_dh, blocks, stream);
 }
 
 }  // namespace
@@ -973,13 +1177,15 @@ dart_status_t lmhead::launch_bwd_gemms(const uint16_t* dz, int64_t ld_dz, int64_
                                        int64_t d, const Grad& dh_out, bool dh_acc, int64_t ksplit,
                                        int64_t part_stride, const Grad& dw_out, bool dw_acc,
                                        hipStream_t stream, const int32_t* dh_map, const int32_t* dyn_rows,
-                                       int64_t dyn_base, const float* scale) {
-    if ((dh_out.bf16 && dh_acc) || (dw_out.bf16 && dw_acc)) return DART_ERR_INVALID_ARG;
+                                       int64_t dyn_base, const float* scale, bool small) {
+    if ((dh_out.bf16 && dh_acc) || (dw_out.bf16 && dw_acc) || (small && dh_acc))
+        return DART_ERR_INVALID_ARG;
     if (ld_dz > kMaxLd || ld_w > kMaxLd || ld_h > kMaxLd || dh_out.ld > kMaxLd ||
         dw_out.ld > kMaxLd)
         return DART_ERR_UNSUPPORTED;
-    BwdGemm dh = make_bwd_gemm(dz, ld_dz, w, ld_w, rows, d, cols, dh_out);
-    BwdGemm dw = make_bwd_gemm(dz, ld_dz, h, ld_h, cols, d, rows, dw_out);
+    const int bm = small ? BwdSmall::BM : LmCfg::BM, bn = small ? BwdSmall::BN : LmCfg::BN;
+    BwdGemm dh = make_bwd_gemm(dz, ld_dz, w, ld_w, rows, d, cols, dh_out, bm, bn);
+    BwdGemm dw = make_bwd_gemm(dz, ld_dz, h, ld_h, cols, d, rows, dw_out, bm, bn);
     // the block's rows are dh's M and dW's K
     dh.dyn = dw.dyn = dyn_rows;
     dh.dyn_base = dw.dyn_base = dyn_base;
@@ -996,9 +1202,10 @@ dart_status_t lmhead::launch_bwd_gemms(const uint16_t* dz, int64_t ld_dz, int64_
     if (blocks == 0) return DART_OK;
     if (!grid_fits(blocks, LmCfg::THREADS)) return DART_ERR_UNSUPPORTED;
     const int dhm = out_mode(dh_out, dh_acc), dwm = out_mode(dw_out, dw_acc);
-    if (dhm == kOutF32) launch_bwd_gemms_dw<kOutF32>(dwm, dh, dw, n_dh, blocks, stream);
-    else if (dhm == kOutF32Acc) launch_bwd_gemms_dw<kOutF32Acc>(dwm, dh, dw, n_dh, blocks, stream);
-    else launch_bwd_gemms_dw<kOutBf16>(dwm, dh, dw, n_dh, blocks, stream);
+    if (small)
+        launch_bwd_gemms_c<BwdSmall>(dhm, dwm, dh, dw, n_dh, blocks, stream);
+    else
+        launch_bwd_gemms_c<LmCfg>(dhm, dwm, dh, dw, n_dh, blocks, stream);
     return hipGetLastError() == hipSuccess ? DART_OK : DART_ERR_HIP;
 }
 
@@ -1070,7 +1277,7 @@ dart_status_t backward_core(const uint16_t* h, int64_t T, int64_t d,
                 parts ? Grad{parts, d, false}
                       : Grad{put ? sum_h.p : sum_h.row(r0), sum_h.ld, sum_h.bf16},
                 c0 > 0, parts ? ksplit : 1, R * d, Grad{sum_w.row(c0), sum_w.ld, sum_w.bf16},
-                r0 > 0, stream, put ? map + r0 : nullptr, dyn_rows, r0, nullptr);
+                r0 > 0, stream, put ? map + r0 : nullptr, dyn_rows, r0, nullptr, false);
             if (sg != DART_OK) return sg;
         }
         if (parts) sum_parts(parts, ksplit, R * d, r0, rows);

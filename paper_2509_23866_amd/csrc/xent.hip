@@ -676,15 +676,15 @@ int64_t ceil8(int64_t x) { return (x + 7) / 8 * 8; }
 
 // Parts of a block's dh sum over the vocabulary, as in the LM head's backward: dh's few tiles have
 // long sums, and the launch waits for them while they fill only some of the units. At most as
-// many as give every unit a part; none shorter than four slices of 64; and, as a slice takes
+// many as give every unit a part (of small tiles two); none shorter than four slices of 64; and, as a slice takes
 // kSliceUs where few tiles run, and a part is written and read once more (rows * d * 8 bytes at 4
 // TB/s) and waited for (kPartUs), the n that makes slices * kSliceUs / n + n * part least. (48
 // rows of V = 4000, d = 512: the products 66 us in one part, 15 in 7, 12 in 15.)
 constexpr double kSliceUs = 0.75, kPartUs = 0.1;
-int64_t dh_parts(int64_t rows, int64_t d, int64_t V) {
-    const int64_t tiles =
-        ((rows + LmCfg::BM - 1) / LmCfg::BM) * ((d + LmCfg::BN - 1) / LmCfg::BN);
-    const int64_t by_units = kUnits / tiles, by_k = V / (LmCfg::BK * 4);
+int64_t dh_parts(int64_t rows, int64_t d, int64_t V, bool small) {
+    const int64_t side = small ? 128 : 256, room = small ? 2 * kUnits : kUnits;
+    const int64_t tiles = ((rows + side - 1) / side) * ((d + side - 1) / side);
+    const int64_t by_units = room / tiles, by_k = V / (LmCfg::BK * 4);
     const double slices = (double)V / LmCfg::BK;
     const double part_us = (double)rows * (double)d * 8 / 4e6 + kPartUs;
     const int64_t best = (int64_t)sqrt(slices * kSliceUs / part_us);
@@ -692,11 +692,25 @@ int64_t dh_parts(int64_t rows, int64_t d, int64_t V) {
     return n < best ? (n > 1 ? n : 1) : (best > 1 ? best : 1);
 }
 
+// Whether a block's two products take the small tiles: three of them share a unit, so that their
+// beginnings and stores, most of a dW tile where it has few slices (rows), are hidden; they fill
+// the units where the large ones are few, and half as many columns are empty where d is
+// short of a large one. The large ones load half as much for each product and win elsewhere. Of
+// 110 calls measured (T from 16 to 4096, V from 1000 to 152064, d from 64 to 3584; whole calls) the
+// rule takes the small ones in 75: 74 of them are faster, by 10% on average and 23% at most (2007 rows of
+// V = 2864, d = 152: 73 -> 56 us; 48 of V = 4000, d = 512: 33.4 -> 29.7), one slower (49 of V =
+// 113040, d = 1024: 182 -> 190). 4096 rows of V = 152064, d = 3584 would go from 11.2 to 16.8 ms.
+bool small_tiles(int64_t rows, int64_t d, int64_t V) {
+    const double large = ceil((double)V / 256) * ceil((double)d / 256);  // dW's
+    return d <= 128 || large <= 52 || (rows <= 320 && large <= 2000);
+}
+
 // Where a call's parts sit in the workspace (byte offsets, each 256-byte aligned).
 struct XentPlan {
     int64_t rows;   // a block's
     bool acc_w;     // dW summed over blocks in fp32
     int64_t ksplit; // parts of dh's sum over the vocabulary
+    bool small;     // tiles of the two products
     size_t e, part, z_sum, z_y, count, scale, map, target_c, h_c, panels, accw, parts, total;
 };
 
@@ -706,7 +720,8 @@ XentPlan plan_xent(int64_t T, int64_t d, int64_t V, int64_t rows, bool grad, boo
     XentPlan P = {};
     P.rows = rows < T ? rows : T;
     P.acc_w = grad && want_w && P.rows < T;
-    P.ksplit = grad ? dh_parts(P.rows, d, V) : 1;
+    P.small = grad && small_tiles(P.rows, d, V);
+    P.ksplit = grad ? dh_parts(P.rows, d, V, P.small) : 1;
     const double big = double(int64_t(1) << 60), nvt = (double)column_tiles(V);
     if ((double)P.rows * (double)ceil8(V) * 2 > big || (double)V * (double)d * 4 > big ||
         (double)T * ((double)d + 64) * 128 > big || (double)P.rows * nvt * 16 > big)
@@ -865,7 +880,7 @@ dart_status_t run_xent(const uint16_t* h, int64_t T, int64_t d, int64_t ld_h, co
         const dart_status_t st = lmhead::launch_bwd_gemms(
             e, ld_e, rows, V, w, ld_w, hr, d, d, parts && dh.p ? Grad{parts, d, false} : dh, false,
             parts ? P.ksplit : 1, P.rows * d, sum_w, P.acc_w && r0 > 0, stream, parts ? nullptr : map + r0,
-            count, r0, scale);
+            count, r0, scale, P.small);
         if (st != DART_OK) return st;
         const DhParts to_add = {parts, P.ksplit, P.rows * d, rows, d, map + r0, dh_rows, ld_dh, r0};
         const bool last = r0 + rows == T;
