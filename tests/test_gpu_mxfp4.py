@@ -240,6 +240,29 @@ def test_tok_stats_shapes(T, d, V, inv_temp):
         assert np.array_equal(g.cpu().numpy(), a.cpu().numpy())
 
 
+# heights of 256 rows, the last of which has 1, 44, 88, 128 or 129 of them (up to 128 it is formed
+# as a short one), from one to several rounds of the ring; the values from the inverse
+@pytest.mark.parametrize("T,d,V", [(257, 1100, 40000), (300, 64, 30000), (600, 776, 20000),
+                                   (384, 40, 33000), (385, 300, 33000)])
+def test_heights_of_256_rows(T, d, V):
+    import torch
+
+    dart = _dart()
+    rng = np.random.default_rng(T + d + V)
+    qh = dart.dart_mxfp4_quantize(_cuda(rng.normal(size=(T, d)).astype(np.float32)))
+    qw = dart.dart_mxfp4_quantize(_cuda((rng.normal(size=(V, d)) * 3.0 / math.sqrt(d)).astype(np.float32)))
+    y = rng.integers(0, V, T).astype(np.int32)
+    h, w = (dart.dart_mxfp4_dequantize(q, dtype=torch.float32).double().cpu().numpy() for q in (qh, qw))
+    z = h @ w.T
+    tol = d * 2.0 ** -23 * (np.abs(h) @ np.abs(w).T)
+    out = dart.dart_mxfp4_matmul(qh, qw, dtype=torch.float32).double().cpu().numpy()
+    assert np.all(np.abs(out - z) <= tol)
+    out = dart.dart_mxfp4_matmul(qh, qw).double().cpu().numpy()
+    assert np.all(np.abs(out - z) <= tol + 2.0 ** -8 * np.abs(z))
+    for g, r in zip(dart.dart_lmhead_mxfp4_tok_stats(qh, qw, _cuda(y)), _stats_ref(z, y)):
+        assert np.abs(g.cpu().numpy().astype(np.float64) - r).max() <= H.LOGP_TOL
+
+
 def test_tok_stats_of_blocks_that_are_not_finite():
     """A NaN block of a hidden row shows in that row alone, one of a weight row in every row."""
     import torch

@@ -114,6 +114,42 @@ def test_shapes(T, d, V, eps, lam, reduction):
     _check_grads(dh, dw, ref, h, w, y, reduction)
 
 
+# heights of 256 rows, the last of which has 1, 44, 88, 128 or 129 of them (up to 128 it is formed
+# as a short one), from one to several rounds of the ring
+@pytest.mark.parametrize("T,d,V", [(257, 264, 40000), (300, 64, 30000), (600, 520, 20000), (384, 8, 33000),
+                                   (385, 72, 33000)])
+def test_heights_of_256_rows(T, d, V):
+    dart = _dart()
+    h, w, y = _problem(T, d, V, left_out=0.0)
+    ref = ox.xent(h, w, y, 0.1, 1e-3)
+    hd, wd, yd = _dev(h), _dev(w), _ids(y)
+    _check_loss(dart.dart_lmhead_xent_fwd(hd, wd, yd, 0.1, 1e-3), ref, 1e-3)
+    *got, dh, dw = dart.dart_lmhead_xent_fwd_bwd(hd, wd, yd, 0.1, 1e-3)
+    _check_loss(got, ref, 1e-3)
+    _check_grads(dh, dw, ref, h, w, y)
+
+
+# the gradient's products in large and in small tiles (rows, d, V on both sides of the rule), rows and
+# columns that end inside them, blocks of rows, results in wider matrices of odd row lengths
+@pytest.mark.parametrize("T,d,V,chunk,pad", [(321, 136, 15000, 321, 0), (320, 136, 15000, 320, 0),
+                                             (700, 136, 14000, 400, 3), (400, 264, 13569, 400, 1),
+                                             (500, 3584, 1300, 500, 0), (400, 128, 15000, 400, 3),
+                                             (1100, 264, 6700, 350, 0)])
+def test_tiles_of_the_gradient_products(T, d, V, chunk, pad):
+    import torch
+
+    dart = _dart()
+    h, w, y = _problem(T, d, V)
+    ref = ox.xent(h, w, y, 0.1, 1e-3)
+    dh = torch.full((T, d + pad), 7.0, dtype=torch.bfloat16, device="cuda")
+    dw = torch.full((V, d + pad), 7.0, dtype=torch.bfloat16, device="cuda")
+    *got, _, _ = dart.dart_lmhead_xent_fwd_bwd(_dev(h), _dev(w), _ids(y), 0.1, 1e-3, chunk_rows=chunk,
+                                               dhidden=dh[:, :d], dweight=dw[:, :d])
+    _check_loss(got, ref, 1e-3)
+    _check_grads(dh[:, :d], dw[:, :d], ref, h, w, y)
+    assert bool((dh[:, d:] == 7.0).all()) and bool((dw[:, d:] == 7.0).all())
+
+
 @pytest.mark.parametrize("chunk", [1, 100, 256, 300, 512])
 def test_chunks(chunk):
     """dweight summed over chunks of rows, also where the last ones hold no labelled row."""
