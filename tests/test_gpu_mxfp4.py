@@ -263,6 +263,24 @@ def test_heights_of_256_rows(T, d, V):
         assert np.abs(g.cpu().numpy().astype(np.float64) - r).max() <= H.LOGP_TOL
 
 
+@pytest.mark.parametrize("out", ["bf16", "f32"])
+def test_product_of_more_than_32_bits_of_elements(out):
+    """16500 x 152064 results (2.5e9): rows on both sides of 2^31 elements, every column."""
+    import torch
+
+    dart = _dart()
+    g = torch.Generator(device="cuda").manual_seed(9)
+    M, N, K = 16500, 152064, 72
+    qa = dart.dart_mxfp4_quantize(torch.randn((M, K), generator=g, device="cuda"))
+    qb = dart.dart_mxfp4_quantize(torch.randn((N, K), generator=g, device="cuda"))
+    a, b = (dart.dart_mxfp4_dequantize(q, dtype=torch.float32).double() for q in (qa, qb))
+    got = dart.dart_mxfp4_matmul(qa, qb, dtype=torch.bfloat16 if out == "bf16" else torch.float32)
+    for rows in (slice(0, 64), slice(7000, 7100), slice(14100, 14150), slice(16400, 16500)):
+        z, size = a[rows] @ b.t(), a[rows].abs() @ b.abs().t()
+        tol = K * 2.0 ** -23 * size + (2.0 ** -8 * z.abs() if out == "bf16" else 0.0)
+        assert bool(((got[rows].double() - z).abs() <= tol).all())
+
+
 def test_tok_stats_of_blocks_that_are_not_finite():
     """A NaN block of a hidden row shows in that row alone, one of a weight row in every row."""
     import torch

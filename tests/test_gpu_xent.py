@@ -463,6 +463,45 @@ def test_capture_is_refused_beside_any_graph_of_a_leaf():
             assert torch.equal(x, z)
 
 
+def test_offsets_past_32_bits():
+    """16500 rows of V = 152064 in one block: 5 GB of exponentials, and results of rows and entries
+    on both sides of 2^31 elements against a float64 sum on the GPU."""
+    import torch
+
+    dart = _dart()
+    T, d, V = 16500, 64, 152064
+    g = torch.Generator(device="cuda").manual_seed(5)
+    hd = torch.randn((T, d), generator=g, device="cuda").to(torch.bfloat16)
+    wd = (torch.randn((V, d), generator=g, device="cuda") * 0.4).to(torch.bfloat16)
+    yd = torch.randint(0, V, (T,), generator=g, device="cuda", dtype=torch.int32)
+    loss, tok, n, dh, dw = dart.dart_lmhead_xent_fwd_bwd(hd, wd, yd, chunk_rows=T, reduction="sum")
+    h, w, y = hd.double(), wd.double(), yd.long()
+    rdh, mdh = torch.empty_like(h), torch.empty_like(h)
+    rdw, mdw = torch.zeros_like(w), torch.zeros_like(w)
+    ref = torch.empty(T, dtype=torch.float64, device="cuda")
+    for r in range(0, T, 1500):
+        s = slice(r, min(r + 1500, T))
+        z = h[s] @ w.t()
+        lse = torch.logsumexp(z, 1)
+        at = y[s][:, None]
+        ref[s] = lse - z.gather(1, at)[:, 0]
+        p = (z - lse[:, None]).exp_()
+        mdh[s] = p @ w.abs() + w.abs()[y[s]]
+        mdw += p.t() @ h[s].abs()
+        mdw.index_add_(0, y[s], h[s].abs())
+        p.scatter_add_(1, at, torch.full_like(at, -1, dtype=torch.float64))
+        rdh[s] = p @ w
+        rdw += p.t() @ h[s]
+    assert int(n) == T and float((tok.double() - ref).abs().max()) <= H.LOGP_TOL + 2.0 ** -24 * float(ref.max())
+    assert abs(float(loss) - float(ref.sum())) <= H.LOGP_TOL * T + 2.0 ** -23 * float(ref.sum())
+    each = U + 2.0 ** -11 + 2.0 ** -13
+    least = 2.0 ** -39
+    tol = each * mdh + least * w.abs().sum(0) + V * 2.0 ** -24 * mdh + U * rdh.abs()
+    assert bool(((dh.double() - rdh).abs() <= tol).all())
+    tol = each * mdw + least * h.abs().sum(0) + T * 2.0 ** -24 * mdw + U * rdw.abs()
+    assert bool(((dw.double() - rdw).abs() <= tol).all())
+
+
 def test_checks_report_ids_past_the_vocabulary(monkeypatch):
     dart = _dart()
     h, w, y = _problem(20, 16, 50)
