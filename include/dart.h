@@ -561,7 +561,8 @@ size_t dart_lmhead_backward_split_workspace_bytes(int64_t T, int64_t d, int64_t 
                                                   uint32_t flags);
 
 /* ------------------------------------------------------------------------
- * Supervised learning of the LM head: cross entropy and its gradient
+ * Supervised learning of the LM head: cross entropy and its gradient.
+ * Outputs and workspaces lie apart from the inputs and from each other.
  * ------------------------------------------------------------------------ */
 
 /* Reduction of the tokens' losses: over the tokens with a label. */
@@ -652,7 +653,8 @@ dart_status_t dart_grad_scale(void* x, dart_dtype_t dtype, int64_t rows, int64_t
                               const float* factor, hipStream_t stream);
 
 /* ------------------------------------------------------------------------
- * The LM head in four bits (MXFP4)
+ * The LM head in four bits (MXFP4).
+ * Outputs and workspaces lie apart from the inputs and from each other.
  * ------------------------------------------------------------------------ */
 
 /* A quantised R x K matrix: every run of 32 values of a row (the last one of a

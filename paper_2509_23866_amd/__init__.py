@@ -964,6 +964,22 @@ def _out_matrix(name, out, shape, dtype, device):
     return out
 
 
+def _span(t):
+    """The addresses [first, end) between which a matrix or a vector lies."""
+    last = (t.shape[0] - 1) * t.stride(0) + t.shape[1] if t.ndim == 2 else t.numel()
+    return t.data_ptr(), t.data_ptr() + last * t.element_size()
+
+
+def _check_apart(**tensors):
+    """Refuses outputs (the first of each pair) that share memory with what the call still reads."""
+    for names, (out, other) in tensors.items():
+        if out is None or other is None:
+            continue
+        (a, a_end), (b, b_end) = _span(out), _span(other)
+        if a < b_end and b < a_end:
+            raise ValueError("the memory of {} and {} must not overlap".format(*names.split("_and_")))
+
+
 def _ld(t):
     """The row stride of a matrix (of one row: its length)."""
     return t.stride(0) if t.shape[0] > 1 else t.shape[1]
@@ -1052,7 +1068,8 @@ def dart_lmhead_xent_fwd_bwd(hidden, weight, target, label_smoothing=0.0, z_loss
     """dart_lmhead_xent_fwd's (loss, tok_loss, n_valid) and the loss's gradients (dhidden [T, d],
     dweight [V, d]) in bfloat16, the logits formed once: chunk_rows rows of their exponentials at a
     time are kept in the workspace (default: lmhead_xent_plan's). ``want`` says which gradients to
-    form (None is returned for the other). ``workspace``: "auto" (allocated here) or a uint8 device
+    form (None is returned for the other); ``dhidden`` and ``dweight`` are matrices to write them to,
+    apart from the inputs. ``workspace``: "auto" (allocated here) or a uint8 device
     tensor of dart_lmhead_xent_workspace_bytes(T, d, V, chunk_rows) bytes."""
     want_h, want_w = map(bool, want)
     if not (want_h or want_w):
@@ -1071,6 +1088,9 @@ def dart_lmhead_xent_fwd_bwd(hidden, weight, target, label_smoothing=0.0, z_loss
     chunk_rows = lmhead_xent_plan(T, V) if chunk_rows is None else max(1, min(int(chunk_rows), T))
     dhidden = _out_matrix("dhidden", dhidden, (T, d), bf16, dev) if want_h else None
     dweight = _out_matrix("dweight", dweight, (V, d), bf16, dev) if want_w else None
+    _check_apart(dhidden_and_hidden=(dhidden, hidden), dhidden_and_weight=(dhidden, weight),
+                 dweight_and_hidden=(dweight, hidden), dweight_and_weight=(dweight, weight),
+                 dhidden_and_dweight=(dhidden, dweight))
     loss = torch.empty(1, dtype=torch.float32, device=dev)
     tok = torch.empty(T, dtype=torch.float32, device=dev)
     n = torch.empty(1, dtype=torch.int32, device=dev)
@@ -1159,6 +1179,7 @@ def dart_mxfp4_quantize(x, out=None, stream=None):
         _check_mxfp4("out", out, x.device)
         if (out.rows, out.cols) != (R, K):
             raise ValueError(f"out must be {R} x {K}")
+        _check_apart(out_and_x=(out.data, x))
     _enqueue("dart_mxfp4_quantize", x.device, stream, x.data_ptr(), _FLOATS[str(x.dtype)], R, K, ld,
              out.data.data_ptr())
     return out
@@ -1176,6 +1197,7 @@ def dart_mxfp4_dequantize(q, dtype=None, out=None, stream=None):
     if str(dtype) not in _FLOATS:
         raise TypeError("dtype must be float32 or bfloat16")
     out = _out_matrix("out", out, (q.rows, q.cols), dtype, q.data.device)
+    _check_apart(out_and_q=(out, q.data))
     _enqueue("dart_mxfp4_dequantize", out.device, stream, q.data.data_ptr(), q.rows,
              q.cols, _FLOATS[str(dtype)], out.data_ptr(), _ld(out))
     return out
@@ -1223,6 +1245,7 @@ def dart_mxfp4_matmul(a, b, dtype=None, out=None, stream=None):
     dev = b.data.device
     rows = _rows_against("a", a, b)
     out = _out_matrix("out", out, (rows, b.rows), dtype, dev)
+    _check_apart(out_and_a=(out, a.data if isinstance(a, Mxfp4) else a), out_and_b=(out, b.data))
     a = _as_mxfp4(a, stream)
     _enqueue("dart_mxfp4_matmul", dev, stream, a.data.data_ptr(), a.rows, b.data.data_ptr(), b.rows,
              b.cols, _FLOATS[str(dtype)], out.data_ptr(), _ld(out))

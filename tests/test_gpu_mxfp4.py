@@ -431,3 +431,20 @@ def test_refusals_with_tensors():
             dart.dart_lmhead_mxfp4_tok_stats(q, q, y, inv_temp=temp)
     with pytest.raises(dart.DartError):  # too small a workspace
         dart.dart_lmhead_mxfp4_tok_stats(q, q, y, workspace=torch.empty(64, dtype=torch.uint8, device="cuda"))
+
+
+def test_results_apart_from_the_inputs():
+    import torch
+
+    dart = _dart()
+    x = torch.randn((64, 512), device="cuda")
+    q = dart.dart_mxfp4_quantize(x)
+    room = x.view(torch.uint8).reshape(-1)
+    inside = dart.Mxfp4(room[:q.data.numel()], 64, 512)
+    for call in (lambda: dart.dart_mxfp4_quantize(x, out=inside),
+                 lambda: dart.dart_mxfp4_dequantize(inside, out=x),
+                 lambda: dart.dart_mxfp4_matmul(inside, q, out=x[:, :64]),
+                 lambda: dart.dart_mxfp4_matmul(q, inside, out=x[:, :64]),
+                 lambda: dart.dart_mxfp4_matmul(x, q, out=x[:, :64])):
+        with pytest.raises(ValueError, match="overlap"):
+            call()

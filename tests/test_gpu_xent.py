@@ -544,3 +544,19 @@ def test_refusals_with_tensors():
         dart.dart_grad_scale(hd, torch.ones(2, device="cuda"))
     with pytest.raises(ValueError):
         dart.dart_grad_scale(hd, 2.0)
+
+
+def test_results_apart_from_the_inputs():
+    import torch
+
+    dart = _dart()
+    h, w, y = _problem(20, 16, 50)
+    hd, wd, yd = _dev(h), _dev(w), _ids(y)
+    both = torch.empty((69, 16), dtype=torch.bfloat16, device="cuda")
+    for kw in (dict(dhidden=hd), dict(dweight=wd), dict(dhidden=both[:20], dweight=both[19:])):
+        with pytest.raises(ValueError, match="overlap"):
+            dart.dart_lmhead_xent_fwd_bwd(hd, wd, yd, **kw)
+    both = torch.empty((70, 16), dtype=torch.bfloat16, device="cuda")
+    got = dart.dart_lmhead_xent_fwd_bwd(hd, wd, yd, dhidden=both[:20], dweight=both[20:])
+    for a, b in zip(got, dart.dart_lmhead_xent_fwd_bwd(hd, wd, yd)):
+        assert torch.equal(a, b)
