@@ -264,13 +264,12 @@ struct Cfg4 {
     static constexpr int BM = BM_, BN = 128, WM = WM_, WN = WN_, NS = NS_;
     static constexpr int WAVES = 4, THREADS = 256;
     static constexpr int TM = BM / WM / 32, TN = BN / WN / 32;  // MFMA tiles per wave
-    static constexpr int SETS = TM == 1 ? 2 : 1;  // of registers for A's panels
+    static constexpr int SETS = NS % 2 == 0 ? 2 : 1;  // of registers for A's panels
     static constexpr int RS = WM * 32;  // rows between a wave's row blocks
     static constexpr int RUNS = BN / 32;  // panels of B a slice: one for each wave to bring
     static constexpr int CROW = BN + 4, CROW16 = BN + 8;  // as in Cfg
     static_assert(WM * WN == WAVES && RUNS == WAVES && TM * WM * 32 == BM && TN * WN * 32 == BN,
                   "four waves");
-    static_assert(SETS == 1 || NS % 2 == 0, "a slice's set goes by its buffer");
     struct alignas(16) Smem {
         union {
             uint8_t b[NS][RUNS][kPanel];
@@ -281,11 +280,13 @@ struct Cfg4 {
     };
     static_assert(sizeof(Smem) <= 80 * 1024, "two workgroups per compute unit");
 };
-// 256 rows; fewer for few rows, with more slices in flight where B comes from HBM and little
-// is multiplied per byte of it.
+// 256 rows; fewer for few rows, where B comes from HBM and little is multiplied per byte of it. 128
+// rows with a slice more in flight (and its set of registers): 128 rows of V = 152064, d = 3584
+// 61 us to 70. 64 rows with three workgroups a unit in its place: 64 rows of V = 152064, d = 1024 22.4
+// us to 24.7, 48 x 32003 of K = 2056 13.6 to 14.1, d = 3584 66.8 to 66.2.
 using Mx256 = Cfg4<256, 4, 1, 3>;
 using Mx128 = Cfg4<128, 4, 1, 4>;
-using Mx64 = Cfg4<64, 2, 2, 4>;
+using Mx64 = Cfg4<64, 2, 2, 3>;
 
 // The operands of a product: panels, and panels per row of panels.
 struct Mxfp4Pair {
