@@ -191,6 +191,30 @@ def test_no_labels_one_label_and_ids_past_the_vocabulary(T):
     torch.cuda.synchronize()
 
 
+@pytest.mark.parametrize("T", [1, 2, 63, 64, 65, 300])
+def test_the_sum_of_the_rows_losses(T):
+    """The loss is the float64 sum of tok_loss, rounded once (where its order may change no more
+    than the last bit), the same bits every time, also over a workspace that held anything."""
+    import torch
+
+    dart = _dart()
+    h, w, y = _problem(T, 72, 700, left_out=0.4, seed=T)
+    y[T // 2] = 5
+    hd, wd = _dev(h), _dev(w)
+    n = dart.dart_lmhead_xent_fwd_workspace_bytes(T, 72, 700)
+    for labels in (y, np.where(np.arange(T) == T - 1, 3, -100), np.full(T, -100)):
+        yd = _ids(labels)
+        for reduction in ("mean", "sum"):
+            first = None
+            for fill in (0, 255, 1, 77, 255, 0):
+                ws = torch.full((n,), fill, dtype=torch.uint8, device="cuda")
+                loss, tok, _ = dart.dart_lmhead_xent_fwd(hd, wd, yd, reduction=reduction, workspace=ws)
+                want = _np(tok).sum() / (max((labels >= 0).sum(), 1) if reduction == "mean" else 1)
+                assert abs(float(loss) - want) <= 2.0 ** -23 * abs(want)
+                first = loss if first is None else first
+                assert torch.equal(loss, first)
+
+
 def test_rows_left_out_may_hold_anything():
     """NaNs and infinities in the hidden states of rows without a label reach nothing, and the
     same rows' outputs are zeros."""
