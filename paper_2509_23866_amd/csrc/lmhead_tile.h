@@ -184,7 +184,7 @@ __device__ __forceinline__ Triple merge(const Triple& a, const Triple& b) {
 // as its first operand, so that a lane holds 16 TN columns of one row, four
 // adjacent ones in consecutive registers. (With A's rows first a lane holds
 // one column of 16 rows, and every epilogue had to turn the fp32 tile round in
-// LDS, one value at a time. Measured at d = 3584, V = 152064, the same box:
+// LDS, one value at a time. Measured at d = 3584, V = 152064, the same card:
 // statistics 3450 -> 3378 us at T = 4096 and 950 -> 925 at 1000, the backward
 // with bf16 gradients 10702 -> 10565 and 2953 -> 2856, dlogits 928 -> 917 at
 // 1000, the fp32 gradients within 0.3%.) Ends on a barrier with no loads in
