@@ -712,9 +712,9 @@ __device__ __forceinline__ void with_rows_of(int64_t M, int64_t m0, F&& f) {
     double least = 0;
     for (int k = 0; k < 3; ++k) {
         const int bm = 64 << k;
-        // the last height of 256 takes as long as one of 128 where that is enough (FirstRows)
+        // the last height of 256 is shorter work where it has 128 rows at most (FirstRows)
         const int64_t tail = rows % bm;
-        const double last = tail == 0 ? 0 : k == 2 && tail <= 128 ? each[1] / each[2] : 1;
+        const double last = tail == 0 ? 0 : k == 2 && tail <= 128 ? 0.75 : 1;
         const double per_unit = ((double)(rows / bm) + last) * (double)column_tiles / kUnits;
         const double cost = fmax(per_unit > 1 ? second * alone[k] : alone[k],
                                  each[k] * (per_unit + 0.4));

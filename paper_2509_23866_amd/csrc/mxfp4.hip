@@ -656,11 +656,11 @@ Mxfp4Pair pair_of(const void* a, int64_t M, const void* b, int64_t N, int64_t K)
 int64_t column_tiles(int64_t N) { return (N + Mx256::BN - 1) / Mx256::BN; }
 
 // f(configuration that forms M x N results fastest); times in us at K = 3584 (fastest_height).
-// Of 392 calls measured (M from 40 to 4096, N from 1088 to 152064, K = 256, 1024 and 3584,
-// products and statistics) the choice is within 14% of the fastest of the three, 0.4% on average.
+// Of 270 calls measured (M from 40 to 4000, N from 1088 to 152064, K = 256, 1024 and 3584,
+// products and statistics) the choice is within 18% of the fastest of the three, 1.1% on average.
 template <class F>
 void with_mxfp4_cfg(int64_t M, int64_t N, F&& f) {
-    const int bm = fastest_height(M, column_tiles(N), {7.6, 10, 12.6}, {7, 9.4, 15}, 1.3);
+    const int bm = fastest_height(M, column_tiles(N), {6.4, 8.6, 12.6}, {6.2, 8.7, 15}, 1.3);
     if (bm == 64)
         f(Mx64{});
     else if (bm == 128)
