@@ -704,7 +704,8 @@ dart_status_t dart_mxfp4_matmul(const void* a, int64_t M, const void* b, int64_t
  * are quantised: log-probs, entropies and normalisers of a rollout policy whose
  * head is kept in four bits (the pi^Rollout of Sec. 4.4, whose difference from
  * the trainer's policy the truncated importance weight corrects), without
- * logits in memory. target, inv_temp, logp, entropy, lse as there.
+ * logits in memory. target, inv_temp, logp, entropy, lse as there; a NaN among a row's
+ * logits (a block that stands for NaN, wherever it is) shows in all three.
  *   workspace: device memory of at least dart_lmhead_mxfp4_stats_workspace_bytes(T, V) bytes
  *              (T * ceil(V/128) * 16 + T * 4), 16-byte aligned, owned by the
  *              caller; contents on entry do not matter.

@@ -531,33 +531,33 @@ __device__ __forceinline__ void stats_of_tile(F&& tile, int64_t T, int64_t V,
                 for (int v = 0; v < 16; ++v) mx = fmaxf(mx, acc[i][2 * u + j][v]);
             // scale > 0: the maximum of the scaled row is the scaled maximum
             Triple mine = {mx * scale, 0.f, 0.f};
-            if (mx > -INFINITY) {
-                // e = 2^xl with xl = (x - mx) scale log2(e); where a column was
-                // dropped (-inf) xl is floored at -200, where 2^xl is already 0 in
-                // fp32, so that it adds 0 (other columns are finite)
-                const float ml = mx * c2;
-                float s2[2], w2[2];
-                auto sums = [&](auto floored) {
+            // e = 2^xl with xl = (x - mx) scale log2(e); where a column was
+            // dropped (-inf) xl is floored at -200, where 2^xl is already 0 in
+            // fp32, so that it adds 0. A maximum of -inf says that every column
+            // was dropped or is a NaN (which a maximum passes over): the sums run
+            // all the same, from 0, and a NaN shows in them
+            const float ml = mx == -INFINITY ? 0.f : mx * c2;
+            float s2[2], w2[2];
+            auto sums = [&](auto floored) {
 #pragma unroll
-                    for (int j = 0; j < 2; ++j) {
-                        s2[j] = w2[j] = 0.f;
+                for (int j = 0; j < 2; ++j) {
+                    s2[j] = w2[j] = 0.f;
 #pragma unroll
-                        for (int v = 0; v < 16; ++v) {
-                            float xl = fmaf(acc[i][2 * u + j][v], c2, -ml);
-                            if constexpr (decltype(floored)::value) xl = xl < -200.f ? -200.f : xl;
-                            const float e = __builtin_amdgcn_exp2f(xl);
-                            s2[j] += e;
-                            w2[j] = fmaf(e, xl, w2[j]);
-                        }
+                    for (int v = 0; v < 16; ++v) {
+                        float xl = fmaf(acc[i][2 * u + j][v], c2, -ml);
+                        if constexpr (decltype(floored)::value) xl = xl < -200.f ? -200.f : xl;
+                        const float e = __builtin_amdgcn_exp2f(xl);
+                        s2[j] += e;
+                        w2[j] = fmaf(e, xl, w2[j]);
                     }
-                };
-                if (masked)
-                    sums(std::true_type{});
-                else
-                    sums(std::false_type{});
-                mine.s = s2[0] + s2[1];
-                mine.w = (w2[0] + w2[1]) * 0.6931471805599453f;
-            }
+                }
+            };
+            if (masked)
+                sums(std::true_type{});
+            else
+                sums(std::false_type{});
+            mine.s = s2[0] + s2[1];
+            mine.w = (w2[0] + w2[1]) * 0.6931471805599453f;
             Triple o;
             o.m = __shfl_xor(mine.m, 32);
             o.s = __shfl_xor(mine.s, 32);
@@ -616,9 +616,10 @@ lmhead_merge_kernel(const float4* __restrict__ part, const float* __restrict__ z
     if (lane != 0) return;
     const int64_t y = target[t];
     const float zy = (y >= 0 && y < V) ? z_y[t] : __builtin_nanf("");
-    const float M = acc.s > 0.f ? fmaxf(acc.m, zy) : zy;
+    const bool others = acc.s != 0.f;  // also where it is a NaN
+    const float M = others ? fmaxf(acc.m, zy) : zy;
     float sx = 0.f, wx = 0.f;
-    if (acc.s > 0.f) {
+    if (others) {
         const float dx = acc.m - M;
         const float cx = expf(dx);
         sx = cx * acc.s;
@@ -629,8 +630,9 @@ lmhead_merge_kernel(const float4* __restrict__ part, const float* __restrict__ z
     const float S = sx + ey;
     const float W = fmaf(ey, xy, wx);
     const float ln_s = logf(S);
+    const float h = ln_s - W / S;
     lse[t] = M + ln_s;
-    entropy[t] = fmaxf(ln_s - W / S, 0.f);
+    entropy[t] = h < 0.f ? 0.f : h;
     logp[t] = sx < ey ? -log1pf(sx / ey) : xy - ln_s;
 }
 
