@@ -17,11 +17,14 @@ device calls. From the LM head's inputs: ``dart_lmhead_tok_stats`` and
 ``dart_lmhead_backward``; its supervised loss, ``dart_lmhead_xent_fwd`` and, with
 the gradients, ``dart_lmhead_xent_fwd_bwd``; and the head in four bits,
 ``dart_mxfp4_quantize`` (an ``Mxfp4``), ``dart_mxfp4_dequantize``,
-``dart_mxfp4_matmul`` and ``dart_lmhead_mxfp4_tok_stats``.
+``dart_mxfp4_matmul`` and ``dart_lmhead_mxfp4_tok_stats``. With ``stream`` these last
+two sets run as under ``torch.cuda.stream(stream)``: what they allocate, results
+included, is that stream's.
 """
 
 from __future__ import annotations
 
+import contextlib
 import ctypes
 import importlib
 import os
@@ -930,26 +933,26 @@ def lmhead_backward_plan(T: int, V: int, budget_bytes: int = 512 << 20):
     return best[1], best[2]
 
 
-def _enqueue(name, device, stream, *args):
-    """The C call ``name`` on ``stream``, with the inputs' device current: the null stream is the
-    current device's."""
+def _on(stream, device):
+    """A context in which ``stream`` (as _stream_handle takes it) is the current one of ``device``,
+    and that the current device: the null stream is the current device's, and what is allocated in
+    it is handed out, and again after it, in the order of the stream whose kernels use it."""
     torch = _torch()
-    fn = getattr(load_library(), name)
-    if torch.cuda.current_device() == device.index:
-        rc = fn(*args, _stream_handle(stream, device))
-    else:
-        with torch.cuda.device(device):
-            rc = fn(*args, _stream_handle(stream, device))
+    if stream is None:
+        here = torch.cuda.current_device() == device.index
+        return contextlib.nullcontext() if here else torch.cuda.device(device)
+    handle = _stream_handle(stream, device)
+    if not isinstance(stream, torch.cuda.Stream):  # (a handle of 0 would make a new stream)
+        stream = (torch.cuda.ExternalStream(handle, device=device) if handle
+                  else torch.cuda.default_stream(device))
+    return torch.cuda.stream(stream)
+
+
+def _enqueue(name, device, *args):
+    """The C call ``name`` on the current stream of ``device``, inside _on."""
+    rc = getattr(load_library(), name)(*args, _stream_handle(None, device))
     if rc != DART_OK:
         raise DartError(name, rc)
-
-
-def _used_on(stream, *tensors):
-    """Keeps what a call allocated itself from being handed out again before ``stream``, if it is
-    one of torch's, has passed the call."""
-    if stream is not None and hasattr(stream, "cuda_stream"):
-        for t in tensors:
-            t.record_stream(stream)
 
 
 def _out_matrix(name, out, shape, dtype, device):
@@ -985,14 +988,13 @@ def _ld(t):
     return t.stride(0) if t.shape[0] > 1 else t.shape[1]
 
 
-def _byte_workspace(workspace, nbytes, device, stream):
+def _byte_workspace(workspace, nbytes, device):
     """``workspace``, or for "auto" a new uint8 tensor of nbytes."""
     torch = _torch()
     if isinstance(workspace, str):
         if workspace != "auto":
             raise ValueError('workspace must be "auto" or a uint8 device tensor')
         workspace = torch.empty(nbytes, dtype=torch.uint8, device=device)
-        _used_on(stream, workspace)
     if (not isinstance(workspace, torch.Tensor) or workspace.dtype != torch.uint8
             or workspace.device != device or not workspace.is_contiguous()):
         raise ValueError("workspace must be a contiguous uint8 tensor on the device of the inputs")
@@ -1052,13 +1054,15 @@ def dart_lmhead_xent_fwd(hidden, weight, target, label_smoothing=0.0, z_loss=0.0
             return _made(out, "dart_lmhead_xent_fwd")
     torch = _torch()
     dev, T, d, V, config = _xent_inputs(hidden, weight, target, label_smoothing, z_loss, reduction)
-    loss = torch.empty(1, dtype=torch.float32, device=dev)
-    tok = torch.empty(T, dtype=torch.float32, device=dev)
-    n = torch.empty(1, dtype=torch.int32, device=dev)
-    workspace = _byte_workspace(workspace, dart_lmhead_xent_fwd_workspace_bytes(T, d, V), dev, stream)
-    _enqueue("dart_lmhead_xent_fwd", dev, stream, hidden.data_ptr(), T, d, _ld(hidden),
-             weight.data_ptr(), V, _ld(weight), target.data_ptr(), ctypes.byref(config),
-             loss.data_ptr(), tok.data_ptr(), n.data_ptr(), workspace.data_ptr(), workspace.numel())
+    with _on(stream, dev):
+        loss = torch.empty(1, dtype=torch.float32, device=dev)
+        tok = torch.empty(T, dtype=torch.float32, device=dev)
+        n = torch.empty(1, dtype=torch.int32, device=dev)
+        workspace = _byte_workspace(workspace, dart_lmhead_xent_fwd_workspace_bytes(T, d, V), dev)
+        _enqueue("dart_lmhead_xent_fwd", dev, hidden.data_ptr(), T, d, _ld(hidden),
+                 weight.data_ptr(), V, _ld(weight), target.data_ptr(), ctypes.byref(config),
+                 loss.data_ptr(), tok.data_ptr(), n.data_ptr(), workspace.data_ptr(),
+                 workspace.numel())
     return loss, tok, n
 
 
@@ -1086,21 +1090,22 @@ def dart_lmhead_xent_fwd_bwd(hidden, weight, target, label_smoothing=0.0, z_loss
     dev, T, d, V, config = _xent_inputs(hidden, weight, target, label_smoothing, z_loss, reduction)
     bf16 = torch.bfloat16
     chunk_rows = lmhead_xent_plan(T, V) if chunk_rows is None else max(1, min(int(chunk_rows), T))
-    dhidden = _out_matrix("dhidden", dhidden, (T, d), bf16, dev) if want_h else None
-    dweight = _out_matrix("dweight", dweight, (V, d), bf16, dev) if want_w else None
-    _check_apart(dhidden_and_hidden=(dhidden, hidden), dhidden_and_weight=(dhidden, weight),
-                 dweight_and_hidden=(dweight, hidden), dweight_and_weight=(dweight, weight),
-                 dhidden_and_dweight=(dhidden, dweight))
-    loss = torch.empty(1, dtype=torch.float32, device=dev)
-    tok = torch.empty(T, dtype=torch.float32, device=dev)
-    n = torch.empty(1, dtype=torch.int32, device=dev)
-    workspace = _byte_workspace(workspace, dart_lmhead_xent_workspace_bytes(T, d, V, chunk_rows),
-                                dev, stream)
-    _enqueue("dart_lmhead_xent_fwd_bwd", dev, stream, hidden.data_ptr(), T, d, _ld(hidden),
-             weight.data_ptr(), V, _ld(weight), target.data_ptr(), ctypes.byref(config),
-             loss.data_ptr(), tok.data_ptr(), n.data_ptr(), _ptr(dhidden),
-             _ld(dhidden) if want_h else 0, _ptr(dweight), _ld(dweight) if want_w else 0, chunk_rows,
-             workspace.data_ptr(), workspace.numel())
+    with _on(stream, dev):
+        dhidden = _out_matrix("dhidden", dhidden, (T, d), bf16, dev) if want_h else None
+        dweight = _out_matrix("dweight", dweight, (V, d), bf16, dev) if want_w else None
+        _check_apart(dhidden_and_hidden=(dhidden, hidden), dhidden_and_weight=(dhidden, weight),
+                     dweight_and_hidden=(dweight, hidden), dweight_and_weight=(dweight, weight),
+                     dhidden_and_dweight=(dhidden, dweight))
+        loss = torch.empty(1, dtype=torch.float32, device=dev)
+        tok = torch.empty(T, dtype=torch.float32, device=dev)
+        n = torch.empty(1, dtype=torch.int32, device=dev)
+        nbytes = dart_lmhead_xent_workspace_bytes(T, d, V, chunk_rows)
+        workspace = _byte_workspace(workspace, nbytes, dev)
+        _enqueue("dart_lmhead_xent_fwd_bwd", dev, hidden.data_ptr(), T, d, _ld(hidden),
+                 weight.data_ptr(), V, _ld(weight), target.data_ptr(), ctypes.byref(config),
+                 loss.data_ptr(), tok.data_ptr(), n.data_ptr(), _ptr(dhidden),
+                 _ld(dhidden) if want_h else 0, _ptr(dweight), _ld(dweight) if want_w else 0,
+                 chunk_rows, workspace.data_ptr(), workspace.numel())
     return loss, tok, n, dhidden, dweight
 
 
@@ -1116,8 +1121,9 @@ def dart_grad_scale(x, factor, stream=None):
     if (not isinstance(factor, torch.Tensor) or factor.dtype != torch.float32
             or factor.device != x.device or factor.numel() != 1):
         raise ValueError(f"factor must be a float32 tensor of one element on {x.device}")
-    _enqueue("dart_grad_scale", x.device, stream, x.data_ptr(), _FLOATS[str(x.dtype)], x.shape[0],
-             x.shape[1], _ld(x), factor.data_ptr())
+    with _on(stream, x.device):
+        _enqueue("dart_grad_scale", x.device, x.data_ptr(), _FLOATS[str(x.dtype)], x.shape[0],
+                 x.shape[1], _ld(x), factor.data_ptr())
     return x
 
 
@@ -1173,15 +1179,16 @@ def dart_mxfp4_quantize(x, out=None, stream=None):
     ld = _ld(x)
     if ld < K:
         raise ValueError("the rows of x must not overlap")
-    if out is None:
-        out = Mxfp4(torch.empty(dart_mxfp4_bytes(R, K), dtype=torch.uint8, device=x.device), R, K)
-    else:
+    if out is not None:
         _check_mxfp4("out", out, x.device)
         if (out.rows, out.cols) != (R, K):
             raise ValueError(f"out must be {R} x {K}")
         _check_apart(out_and_x=(out.data, x))
-    _enqueue("dart_mxfp4_quantize", x.device, stream, x.data_ptr(), _FLOATS[str(x.dtype)], R, K, ld,
-             out.data.data_ptr())
+    with _on(stream, x.device):
+        if out is None:
+            out = Mxfp4(torch.empty(dart_mxfp4_bytes(R, K), dtype=torch.uint8, device=x.device), R, K)
+        _enqueue("dart_mxfp4_quantize", x.device, x.data_ptr(), _FLOATS[str(x.dtype)], R, K, ld,
+                 out.data.data_ptr())
     return out
 
 
@@ -1196,10 +1203,11 @@ def dart_mxfp4_dequantize(q, dtype=None, out=None, stream=None):
     dtype = (torch.bfloat16 if out is None else out.dtype) if dtype is None else dtype
     if str(dtype) not in _FLOATS:
         raise TypeError("dtype must be float32 or bfloat16")
-    out = _out_matrix("out", out, (q.rows, q.cols), dtype, q.data.device)
-    _check_apart(out_and_q=(out, q.data))
-    _enqueue("dart_mxfp4_dequantize", out.device, stream, q.data.data_ptr(), q.rows,
-             q.cols, _FLOATS[str(dtype)], out.data_ptr(), _ld(out))
+    with _on(stream, q.data.device):
+        out = _out_matrix("out", out, (q.rows, q.cols), dtype, q.data.device)
+        _check_apart(out_and_q=(out, q.data))
+        _enqueue("dart_mxfp4_dequantize", out.device, q.data.data_ptr(), q.rows,
+                 q.cols, _FLOATS[str(dtype)], out.data_ptr(), _ld(out))
     return out
 
 
@@ -1222,11 +1230,7 @@ def _rows_against(name, x, weight):
 
 def _as_mxfp4(x, stream):
     """``x`` itself where it is an Mxfp4, else (a float32 or bfloat16 matrix) quantised."""
-    if isinstance(x, Mxfp4):
-        return x
-    q = dart_mxfp4_quantize(x, stream=stream)
-    _used_on(stream, q.data)
-    return q
+    return x if isinstance(x, Mxfp4) else dart_mxfp4_quantize(x, stream=stream)
 
 
 def dart_mxfp4_matmul(a, b, dtype=None, out=None, stream=None):
@@ -1244,11 +1248,12 @@ def dart_mxfp4_matmul(a, b, dtype=None, out=None, stream=None):
         raise TypeError("dtype must be float32 or bfloat16")
     dev = b.data.device
     rows = _rows_against("a", a, b)
-    out = _out_matrix("out", out, (rows, b.rows), dtype, dev)
-    _check_apart(out_and_a=(out, a.data if isinstance(a, Mxfp4) else a), out_and_b=(out, b.data))
-    a = _as_mxfp4(a, stream)
-    _enqueue("dart_mxfp4_matmul", dev, stream, a.data.data_ptr(), a.rows, b.data.data_ptr(), b.rows,
-             b.cols, _FLOATS[str(dtype)], out.data_ptr(), _ld(out))
+    with _on(stream, dev):
+        out = _out_matrix("out", out, (rows, b.rows), dtype, dev)
+        _check_apart(out_and_a=(out, a.data if isinstance(a, Mxfp4) else a), out_and_b=(out, b.data))
+        a = _as_mxfp4(a, stream)
+        _enqueue("dart_mxfp4_matmul", dev, a.data.data_ptr(), a.rows, b.data.data_ptr(), b.rows,
+                 b.cols, _FLOATS[str(dtype)], out.data_ptr(), _ld(out))
     return out
 
 
@@ -1269,16 +1274,18 @@ def dart_lmhead_mxfp4_tok_stats(hidden, weight, target, inv_temp=1.0, logp=None,
     dev = weight.data.device
     T, V = _rows_against("hidden", hidden, weight), weight.rows
     _check_vec("target", target, torch.int32, T, dev)
-    logp = torch.empty(T, dtype=torch.float32, device=dev) if logp is None else logp
-    entropy = torch.empty(T, dtype=torch.float32, device=dev) if entropy is None else entropy
-    lse = torch.empty(T, dtype=torch.float32, device=dev) if lse is None else lse
-    for n, v in (("logp", logp), ("entropy", entropy), ("lse", lse)):
-        _check_vec(n, v, torch.float32, T, dev)
-    workspace = _byte_workspace(workspace, dart_lmhead_mxfp4_stats_workspace_bytes(T, V), dev, stream)
-    hidden = _as_mxfp4(hidden, stream)
-    _enqueue("dart_lmhead_mxfp4_tok_stats", dev, stream, hidden.data.data_ptr(), T,
-             weight.data.data_ptr(), V, weight.cols, target.data_ptr(), float(inv_temp), logp.data_ptr(), entropy.data_ptr(),
-             lse.data_ptr(), workspace.data_ptr(), workspace.numel())
+    with _on(stream, dev):
+        logp = torch.empty(T, dtype=torch.float32, device=dev) if logp is None else logp
+        entropy = torch.empty(T, dtype=torch.float32, device=dev) if entropy is None else entropy
+        lse = torch.empty(T, dtype=torch.float32, device=dev) if lse is None else lse
+        for n, v in (("logp", logp), ("entropy", entropy), ("lse", lse)):
+            _check_vec(n, v, torch.float32, T, dev)
+        workspace = _byte_workspace(workspace, dart_lmhead_mxfp4_stats_workspace_bytes(T, V), dev)
+        hidden = _as_mxfp4(hidden, stream)
+        _enqueue("dart_lmhead_mxfp4_tok_stats", dev, hidden.data.data_ptr(), T,
+                 weight.data.data_ptr(), V, weight.cols, target.data_ptr(), float(inv_temp),
+                 logp.data_ptr(), entropy.data_ptr(), lse.data_ptr(), workspace.data_ptr(),
+                 workspace.numel())
     return logp, entropy, lse
 
 
