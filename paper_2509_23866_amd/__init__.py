@@ -973,14 +973,19 @@ def _span(t):
     return t.data_ptr(), t.data_ptr() + last * t.element_size()
 
 
-def _check_apart(**tensors):
-    """Refuses outputs (the first of each pair) that share memory with what the call still reads."""
-    for names, (out, other) in tensors.items():
-        if out is None or other is None:
+def _check_apart(writes, reads):
+    """Refuses a tensor that the call writes (name -> tensor, or None) where it shares memory with
+    another of them or with one that the call reads."""
+    done = [(n, t) for n, t in reads.items() if t is not None]
+    for name, out in writes.items():
+        if out is None:
             continue
-        (a, a_end), (b, b_end) = _span(out), _span(other)
-        if a < b_end and b < a_end:
-            raise ValueError("the memory of {} and {} must not overlap".format(*names.split("_and_")))
+        a, a_end = _span(out)
+        for other_name, other in done:
+            b, b_end = _span(other)
+            if a < b_end and b < a_end:
+                raise ValueError(f"the memory of {name} and {other_name} must not overlap")
+        done.append((name, out))
 
 
 def _ld(t):
@@ -1059,6 +1064,7 @@ def dart_lmhead_xent_fwd(hidden, weight, target, label_smoothing=0.0, z_loss=0.0
         tok = torch.empty(T, dtype=torch.float32, device=dev)
         n = torch.empty(1, dtype=torch.int32, device=dev)
         workspace = _byte_workspace(workspace, dart_lmhead_xent_fwd_workspace_bytes(T, d, V), dev)
+        _check_apart(dict(workspace=workspace), dict(hidden=hidden, weight=weight, target=target))
         _enqueue("dart_lmhead_xent_fwd", dev, hidden.data_ptr(), T, d, _ld(hidden),
                  weight.data_ptr(), V, _ld(weight), target.data_ptr(), ctypes.byref(config),
                  loss.data_ptr(), tok.data_ptr(), n.data_ptr(), workspace.data_ptr(),
@@ -1093,14 +1099,13 @@ def dart_lmhead_xent_fwd_bwd(hidden, weight, target, label_smoothing=0.0, z_loss
     with _on(stream, dev):
         dhidden = _out_matrix("dhidden", dhidden, (T, d), bf16, dev) if want_h else None
         dweight = _out_matrix("dweight", dweight, (V, d), bf16, dev) if want_w else None
-        _check_apart(dhidden_and_hidden=(dhidden, hidden), dhidden_and_weight=(dhidden, weight),
-                     dweight_and_hidden=(dweight, hidden), dweight_and_weight=(dweight, weight),
-                     dhidden_and_dweight=(dhidden, dweight))
         loss = torch.empty(1, dtype=torch.float32, device=dev)
         tok = torch.empty(T, dtype=torch.float32, device=dev)
         n = torch.empty(1, dtype=torch.int32, device=dev)
         nbytes = dart_lmhead_xent_workspace_bytes(T, d, V, chunk_rows)
         workspace = _byte_workspace(workspace, nbytes, dev)
+        _check_apart(dict(dhidden=dhidden, dweight=dweight, workspace=workspace),
+                     dict(hidden=hidden, weight=weight, target=target))
         _enqueue("dart_lmhead_xent_fwd_bwd", dev, hidden.data_ptr(), T, d, _ld(hidden),
                  weight.data_ptr(), V, _ld(weight), target.data_ptr(), ctypes.byref(config),
                  loss.data_ptr(), tok.data_ptr(), n.data_ptr(), _ptr(dhidden),
@@ -1121,6 +1126,7 @@ def dart_grad_scale(x, factor, stream=None):
     if (not isinstance(factor, torch.Tensor) or factor.dtype != torch.float32
             or factor.device != x.device or factor.numel() != 1):
         raise ValueError(f"factor must be a float32 tensor of one element on {x.device}")
+    _check_apart(dict(x=x), dict(factor=factor.reshape(1)))
     with _on(stream, x.device):
         _enqueue("dart_grad_scale", x.device, x.data_ptr(), _FLOATS[str(x.dtype)], x.shape[0],
                  x.shape[1], _ld(x), factor.data_ptr())
@@ -1183,7 +1189,7 @@ def dart_mxfp4_quantize(x, out=None, stream=None):
         _check_mxfp4("out", out, x.device)
         if (out.rows, out.cols) != (R, K):
             raise ValueError(f"out must be {R} x {K}")
-        _check_apart(out_and_x=(out.data, x))
+        _check_apart(dict(out=out.data), dict(x=x))
     with _on(stream, x.device):
         if out is None:
             out = Mxfp4(torch.empty(dart_mxfp4_bytes(R, K), dtype=torch.uint8, device=x.device), R, K)
@@ -1205,7 +1211,7 @@ def dart_mxfp4_dequantize(q, dtype=None, out=None, stream=None):
         raise TypeError("dtype must be float32 or bfloat16")
     with _on(stream, q.data.device):
         out = _out_matrix("out", out, (q.rows, q.cols), dtype, q.data.device)
-        _check_apart(out_and_q=(out, q.data))
+        _check_apart(dict(out=out), dict(q=q.data))
         _enqueue("dart_mxfp4_dequantize", out.device, q.data.data_ptr(), q.rows,
                  q.cols, _FLOATS[str(dtype)], out.data_ptr(), _ld(out))
     return out
@@ -1250,7 +1256,7 @@ def dart_mxfp4_matmul(a, b, dtype=None, out=None, stream=None):
     rows = _rows_against("a", a, b)
     with _on(stream, dev):
         out = _out_matrix("out", out, (rows, b.rows), dtype, dev)
-        _check_apart(out_and_a=(out, a.data if isinstance(a, Mxfp4) else a), out_and_b=(out, b.data))
+        _check_apart(dict(out=out), dict(a=a.data if isinstance(a, Mxfp4) else a, b=b.data))
         a = _as_mxfp4(a, stream)
         _enqueue("dart_mxfp4_matmul", dev, a.data.data_ptr(), a.rows, b.data.data_ptr(), b.rows,
                  b.cols, _FLOATS[str(dtype)], out.data_ptr(), _ld(out))
@@ -1281,6 +1287,9 @@ def dart_lmhead_mxfp4_tok_stats(hidden, weight, target, inv_temp=1.0, logp=None,
         for n, v in (("logp", logp), ("entropy", entropy), ("lse", lse)):
             _check_vec(n, v, torch.float32, T, dev)
         workspace = _byte_workspace(workspace, dart_lmhead_mxfp4_stats_workspace_bytes(T, V), dev)
+        _check_apart(dict(logp=logp, entropy=entropy, lse=lse, workspace=workspace),
+                     dict(hidden=hidden.data if isinstance(hidden, Mxfp4) else hidden,
+                          weight=weight.data, target=target))
         hidden = _as_mxfp4(hidden, stream)
         _enqueue("dart_lmhead_mxfp4_tok_stats", dev, hidden.data.data_ptr(), T,
                  weight.data.data_ptr(), V, weight.cols, target.data_ptr(), float(inv_temp),
