@@ -973,6 +973,20 @@ def _span(t):
     return t.data_ptr(), t.data_ptr() + last * t.element_size()
 
 
+def _share_memory(x, y):
+    """Whether any byte is in both. Columns of one wider matrix lie between each other's rows: with
+    rows equally far apart, their places in a row decide."""
+    (a, a_end), (b, b_end) = _span(x), _span(y)
+    if a >= b_end or b >= a_end:
+        return False
+    if x.ndim == y.ndim == 2 and min(x.shape[0], y.shape[0]) > 1:
+        pitch, wx, wy = (n * t.element_size() for n, t in ((x.stride(0), x), (x.shape[1], x),
+                                                            (y.shape[1], y)))
+        if pitch == y.stride(0) * y.element_size() and max(wx, wy) <= pitch:
+            return (b - a) % pitch < wx or (a - b) % pitch < wy
+    return True
+
+
 def _check_apart(writes, reads):
     """Refuses a tensor that the call writes (name -> tensor, or None) where it shares memory with
     another of them or with one that the call reads."""
@@ -980,10 +994,8 @@ def _check_apart(writes, reads):
     for name, out in writes.items():
         if out is None:
             continue
-        a, a_end = _span(out)
         for other_name, other in done:
-            b, b_end = _span(other)
-            if a < b_end and b < a_end:
+            if _share_memory(out, other):
                 raise ValueError(f"the memory of {name} and {other_name} must not overlap")
         done.append((name, out))
 
