@@ -1031,7 +1031,7 @@ def lmhead_xent_plan(T: int, V: int, budget_bytes: int = 2 << 30) -> int:
     """chunk_rows for dart_lmhead_xent_fwd_bwd: all rows where their exponentials fit
     budget_bytes, else as many whole tiles of 256 as do, the chunks of one size: each chunk reads
     and rewrites the [V, d] sum of dweight."""
-    T, V = int(T), int(V)
+    T, V = int(T), max(int(V), 1)  # (sizes of 0 are the call's to refuse)
     most = max(budget_bytes // (2 * ((V + 7) // 8 * 8)), 256)
     if T <= most:
         return T
