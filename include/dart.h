@@ -636,11 +636,14 @@ dart_status_t dart_lmhead_xent_fwd_bwd(const void* hidden, int64_t T, int64_t d,
                                        hipStream_t stream);
 
 /* Bytes of workspace of the two calls (0 for arguments outside
- * [1, INT32_MAX]). The second is chunk_rows * ceil8(V) * 2 for the
- * exponentials, chunk_rows * ceil(V/128) * 20 for partial sums, V * d * 4 where
- * chunk_rows < T, T * (4 d + 8) for the labelled rows (padded to whole panels of 32 rows and 64
- * columns once), and at most 64 MiB for dhidden's sum in parts where T and d are multiples of
- * 256. Host only. */
+ * [1, INT32_MAX]). Both have, with R rows at a time (all T; chunk_rows, at most T), R * (4 +
+ * ceil(V/128) * 20) for partial sums, T * 8 for the labelled rows' places and targets and
+ * ceil(T/R) * ceil(R/32) * ceil(d/64) * 4096 for their panels of 32 rows and 64 columns, whole ones
+ * for every R rows: T * d * 2 where R divides T and is a multiple of 32 and d of 64, 32 times that
+ * where R is 1, so that chunks of fewer than 32 rows take more memory, not less. The second has
+ * also R * ceil8(V) * 2 for the exponentials, T * d * 2 for the labelled rows once more, V * d * 4
+ * where R < T and at most 64 MiB for dhidden's sum in parts. Every one of these starts at a
+ * multiple of 256 bytes. Host only. */
 size_t dart_lmhead_xent_fwd_workspace_bytes(int64_t T, int64_t d, int64_t V);
 size_t dart_lmhead_xent_workspace_bytes(int64_t T, int64_t d, int64_t V, int64_t chunk_rows);
 
