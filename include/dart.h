@@ -592,8 +592,10 @@ typedef struct {
  *   workspace: device memory of at least
  *              dart_lmhead_xent_fwd_workspace_bytes(T, d, V) bytes, 16-byte
  *              aligned, owned by the caller; contents on entry do not matter.
- * A row's results do not depend on the other rows of the call. NaN or
- * infinite logits show as NaN in the row's loss (and gradient).
+ * A row's results do not depend on the other rows of the call. A NaN or +infinite
+ * logit shows as NaN in the row's loss (and gradient), as do only -infinite ones; one
+ * of -infinity beside finite ones has probability 0, and gives a loss of +infinity where
+ * the learnt distribution reaches it (the target's, or any with label_smoothing > 0).
  * Errors: INVALID_ARG for a null pointer, sizes or alignments that
  * dart_lmhead_tok_stats refuses, a value outside its range in config, or a
  * workspace that is too small; UNSUPPORTED when ceil(T/64) * ceil(V/128) exceeds
@@ -708,7 +710,8 @@ dart_status_t dart_mxfp4_matmul(const void* a, int64_t M, const void* b, int64_t
  * head is kept in four bits (the pi^Rollout of Sec. 4.4, whose difference from
  * the trainer's policy the truncated importance weight corrects), without
  * logits in memory. target, inv_temp, logp, entropy, lse as there; a NaN among a row's
- * logits (a block that stands for NaN, wherever it is) shows in all three.
+ * logits (a block that stands for NaN, wherever it is) shows in all three. Beside a
+ * logit of -infinity (a sum past float32's range) entropy is not defined.
  *   workspace: device memory of at least dart_lmhead_mxfp4_stats_workspace_bytes(T, V) bytes
  *              (T * ceil(V/128) * 16 + T * 4), 16-byte aligned, owned by the
  *              caller; contents on entry do not matter.
