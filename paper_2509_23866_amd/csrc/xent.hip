@@ -18,9 +18,12 @@
 // So three products of T V d instead of the four of a loss whose coefficients only a
 // second pass knows (dart_lmhead_backward): at T = 4096, V = 152064, d = 3584 the kept
 // exponentials cost a read and a write of 1.25 GB, the fourth product took 3.4 ms.
-// What is rounded: e to fp16 (2^-12 of its value down to 2^-29 of its 64 columns' largest, below
-// that 2^-40 of that: little beside the bf16 that follows), dz to bf16 for the
-// matrix cores, as in dart_lmhead_dlogits. dz is kept divided by 1 - eps and not yet by N,
+// What is rounded: e to fp16, by 2^-11 of its value at most (half a step of 11 bits) down to 2^-29
+// of its 64 columns' largest, below that by 2^-40 of that: an eighth of the bf16 rounding that follows,
+// where 32 bits would be twice the bytes to write and read. dz to bf16, by 2^-8 at most, for the matrix
+// cores, as in dart_lmhead_dlogits: the other operand is bf16, and two bf16 of dz would double two of the
+// three products. Gradients are off from 64 bits by 1.8e-3 to 2.0e-3 of their size in the cases
+// measured; a bf16 result's own rounding is 1.7e-3 of it. dz is kept divided by 1 - eps and not yet by N,
 // so that the target's element of an unsure row, the largest of all, is next to -1 and
 // loses nothing by its rounding.
 #include "lmhead_tile.h"
@@ -520,9 +523,14 @@ __device__ __forceinline__ void clear_row(int64_t t, int64_t d, float* __restric
 
 // One workgroup per row t: finds the row's place among the labelled ones by counting the labels
 // before it, and places or clears it; the first workgroup counts them all. For few rows
-// (kFewRows): 3.2 us at T = 48, 4.6 at 1000 and 8.6 at 4096 (d = 512; half the rows labelled),
-// where the two kernels below take 5.0, 5.8 and 9.7 and are a launch more, about 5 us where the
-// launches bound the call; d = 3584: 4.0, 7.4 and 15.0 to 6.7, 9.3 and 19.3.
+// (kFewRows), as its counting grows with T^2 and a launch less counts in short calls. Half the
+// rows labelled, us by it and by the two kernels below (which are a launch more, about 5 us where
+// the launches bound the call):
+//   T          48          1000         4096          8192          16384          32768
+//   d = 512    3.4  5.3    4.2  5.8     8.8  9.6      13.9  16.0    27.7   26.5    72.0   49.0
+//   d = 3584   3.7  6.6    7.8  9.9     19.0 23.9     35.2  41.8    120    142     198    200
+// They cross between 12288 (20.4 and 22.2 at d = 512) and 32768 rows; kFewRows is well below it, at
+// sizes where the call takes milliseconds and either is within 7 us of the other.
 constexpr int kPrepareThreads = 256;
 constexpr int64_t kFewRows = 4096;
 __global__ void __launch_bounds__(kPrepareThreads)
