@@ -162,28 +162,40 @@ class DartLmHeadXent(torch.autograd.Function):
         return tuple(None if g is None else dart_grad_scale(g, factor) for g in grads) + (None,) * 3
 
 
-def _refuse_mixed_capture(leaves):
-    """torch's engine ends a backward pass by having the stream on which a leaf's gradient
-    accumulator was made wait for it. That node lives as long as any graph of the leaf: under HIP
-    graph capture, one that an eager computation made on another stream would pull that stream into
-    the capture, which ends the process."""
-    for leaf in leaves:
-        made_on = _nat(required=True).accumulator_stream(leaf)
-        if made_on not in (None, torch.cuda.current_stream(leaf.device).stream_id):
-            raise RuntimeError("a graph of this leaf that was made on another stream is still alive: "
+def _captured(stream_id, device):
+    """Whether the stream of this id is being captured (the default stream, of id 0, cannot be)."""
+    kind = torch.cuda.current_stream(device)
+    if stream_id in (0, kind.stream_id):
+        return stream_id != 0
+    with torch.cuda.stream(torch.cuda.Stream(stream_id=stream_id, device_index=kind.device_index,
+                                             device_type=kind.device_type)):
+        return torch.cuda.is_current_stream_capturing()
+
+
+def _refuse_mixed_capture(tensors):
+    """torch's engine runs a node of a graph on the stream on which it was made, and ends a backward
+    pass by having the stream on which a leaf's gradient accumulator was made wait for it. An
+    accumulator lives as long as any graph of its leaf: under HIP graph capture, a node that an eager
+    computation made on another stream would pull that stream into the capture, which ends the
+    process."""
+    for t in tensors:
+        if not all(_captured(made_on, t.device) for made_on in _nat(required=True).graph_streams(t)):
+            raise RuntimeError("a graph that was made on another stream than the captured one is still "
+                               "alive and is, or shares a leaf with, what this loss is computed from: "
                                "release it (the loss, or whatever else was computed from the leaf) "
-                               "before capturing a backward pass of the leaf")
+                               "before capturing a backward pass")
 
 
 def dart_lmhead_xent_loss(hidden, weight, target, label_smoothing=0.0, z_loss=0.0,
                           reduction="mean", chunk_rows=None):
     """Differentiable cross entropy of the LM head's inputs (see the module docstring);
     arguments as for dart_lmhead_xent_fwd_bwd. Rows with a negative target do not count. Under
-    HIP graph capture no graph of the same leaves made on another stream, such as an eager loss, may
-    be alive (a RuntimeError)."""
+    HIP graph capture hidden and weight are leaves or were computed in the capture, and no other graph
+    of their leaves made on another stream, such as an eager loss, may be alive (a RuntimeError). A
+    backward pass is captured with its loss: torch takes that of an eager one out of the capture."""
     want = tuple(torch.is_grad_enabled() and t.requires_grad for t in (hidden, weight))
-    leaves = [t for t, wanted in zip((hidden, weight), want) if wanted and t.is_leaf and t.is_cuda]
-    if leaves and torch.cuda.is_current_stream_capturing():
-        _refuse_mixed_capture(leaves)
+    learnt = [t for t, wanted in zip((hidden, weight), want) if wanted and t.is_cuda]
+    if learnt and torch.cuda.is_current_stream_capturing():
+        _refuse_mixed_capture(learnt)
     return DartLmHeadXent.apply(hidden, weight, target,
                                 (float(label_smoothing), float(z_loss), reduction, chunk_rows), want)

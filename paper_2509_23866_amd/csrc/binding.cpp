@@ -21,6 +21,11 @@
 #include <torch/csrc/autograd/python_variable.h>
 #include <torch/csrc/autograd/variable.h>
 
+#include <memory>
+#include <set>
+#include <unordered_set>
+#include <vector>
+
 #include "dart.h"
 
 namespace {
@@ -618,15 +623,30 @@ NATIVE(lmhead_mxfp4_tok_stats, 4)
     return st == DART_OK ? tuple(o.logp, o.entropy, o.lse) : failed(place, st);
 NATIVE_END
 
-// The id of the stream on which the tensor's gradient accumulator was made; None where it has
-// none, no graph of the tensor being alive.
-NATIVE(accumulator_stream, 1)
+// The ids of the streams on which the nodes of the graphs that end in the tensor were made, the
+// gradient accumulators of their leaves among them (of a leaf, its accumulator alone, where a graph
+// of it is alive).
+NATIVE(graph_streams, 1)
     if (!THPVariable_Check(a[0])) Py_RETURN_NONE;
-    const auto node = torch::autograd::impl::try_get_grad_accumulator(THPVariable_Unpack(a[0]));
-    if (!node) Py_RETURN_NONE;
-    const std::optional<c10::Stream> s = node->stream();
-    if (!s) Py_RETURN_NONE;
-    return PyLong_FromLongLong(s->id());
+    const Tensor& t = THPVariable_Unpack(a[0]);
+    std::unordered_set<const torch::autograd::Node*> seen;
+    std::set<int64_t> streams;
+    std::vector<std::shared_ptr<torch::autograd::Node>> todo = {
+        t.grad_fn() ? t.grad_fn() : torch::autograd::impl::try_get_grad_accumulator(t)};
+    while (!todo.empty()) {
+        const std::shared_ptr<torch::autograd::Node> node = std::move(todo.back());
+        todo.pop_back();
+        if (!node || !seen.insert(node.get()).second) continue;
+        if (const std::optional<c10::Stream> s = node->stream()) streams.insert(s->id());
+        for (const torch::autograd::Edge& e : node->next_edges()) todo.push_back(e.function);
+    }
+    PyObject* out = PyList_New(0);
+    for (const int64_t id : streams) {
+        PyObject* x = out ? PyLong_FromLongLong(id) : nullptr;
+        if (!x || PyList_Append(out, x) != 0) Py_CLEAR(out);
+        Py_XDECREF(x);
+    }
+    return out;
 NATIVE_END
 
 // open(path): the C functions of the library at path.
@@ -651,7 +671,7 @@ PyMethodDef methods[] = {
     ENTRY(grpo_advantage), ENTRY(step_select_groups), ENTRY(tis_loss_fwd_ex),
     ENTRY(lmhead_tok_stats), ENTRY(lmhead_xent_fwd), ENTRY(lmhead_xent_fwd_bwd),
     ENTRY(mxfp4_quantize), ENTRY(mxfp4_dequantize), ENTRY(mxfp4_matmul),
-    ENTRY(lmhead_mxfp4_tok_stats), ENTRY(accumulator_stream), {"open", open_lib, METH_O, nullptr}, {nullptr, nullptr, 0, nullptr}};
+    ENTRY(lmhead_mxfp4_tok_stats), ENTRY(graph_streams), {"open", open_lib, METH_O, nullptr}, {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module_def = {PyModuleDef_HEAD_INIT, "_native", nullptr, -1, methods,
                           nullptr, nullptr, nullptr, nullptr};
 
