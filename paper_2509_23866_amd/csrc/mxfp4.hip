@@ -257,7 +257,7 @@ __device__ __forceinline__ uint32_t load_scales(__amdgpu_buffer_rsrc_t r, uint32
 // workgroups run per compute unit, so that one multiplies while the other is in its epilogue.
 // T = 4096, V = 152064, d = 3584: the statistics 1.02 ms and the product, which stores 1.25 GB,
 // 1.11 (4.4 and 4.0 PFLOP/s), where both operands through LDS in one workgroup a unit took 1.29 and
-// 1.32. The matrix cores are busy 65% of the cycles at 1.6 GHz, a clock that power has already lowered
+// 1.32. The matrix cores are busy 65% of the cycles at 1.5 to 1.6 GHz, which power has already lowered
 // (the same instruction on registers alone is 94% busy at 1.65 GHz, 6.3 to 6.6 PFLOP/s): so what bounds
 // the tile is taken to be power, as rings of other depths, more waves or stores that pass the caches
 // move it by less than 2%.
