@@ -1091,8 +1091,9 @@ def dart_lmhead_xent_fwd_bwd(hidden, weight, target, label_smoothing=0.0, z_loss
     dweight [V, d]) in bfloat16, the logits formed once: chunk_rows rows of their exponentials at a
     time are kept in the workspace (default: lmhead_xent_plan's; fewer than 32 take more workspace,
     not less). ``want`` says which gradients to form (None is returned for the other); ``dhidden``
-    and ``dweight`` are matrices to write them to, apart from the inputs. ``workspace``: "auto" (allocated here) or a uint8 device
-    tensor of dart_lmhead_xent_workspace_bytes(T, d, V, chunk_rows) bytes."""
+    and ``dweight`` are matrices to write them to, apart from the inputs. ``workspace``: "auto"
+    (allocated here) or a uint8 device tensor of dart_lmhead_xent_workspace_bytes(T, d, V, chunk_rows)
+    bytes."""
     want_h, want_w = map(bool, want)
     if not (want_h or want_w):
         raise ValueError("want at least one gradient")
